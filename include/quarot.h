@@ -31,7 +31,8 @@
  *
  * Conventions for every call:
  *  - Pointers are device pointers (hipMalloc or torch CUDA tensors) unless
- *    stated otherwise, and must be 16-byte aligned.  The caller owns every
+ *    stated otherwise, and must be 16-byte aligned (int32 and float arrays of
+ *    the paged calls: 4).  The caller owns every
  *    buffer, including the workspace; the library never allocates, frees
  *    or keeps pointers, and is reentrant.  Its one piece of mutable global
  *    state is the fixed scratch array of quarot_linear_e3m2_scratch (see
@@ -514,6 +515,135 @@ quarot_status quarot_kv_decode_attention(const quarot_f16 *q, const uint8_t *k_c
                                          int64_t nkv, int64_t s_max, int64_t seq_len,
                                          int64_t head_dim, int64_t group, float sm_scale,
                                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- Rotary positions and the paged KV cache --------------------------------
+ *
+ * A server keeps the cache of many sequences in pools of pages and hands the
+ * next tokens of all of them to each layer at once.  These calls take such a
+ * batch: T token rows, of which rows cu_new[b] .. cu_new[b + 1] - 1 are the new
+ * tokens of sequence b (none, one, or a chunk of a prompt), in order.  Rows
+ * from cu_new[batch] on belong to nobody: they are neither read nor written,
+ * so that a captured graph can serve batches of up to T tokens.
+ *
+ * Rotary positions (in the attention block of §4 Stage 1d they come before the
+ * head-wise Hadamard).  Pair f < rot_dim / 2 of a head row is the elements
+ * (f, f + rot_dim / 2), or (2 f, 2 f + 1) with `interleaved`; elements from
+ * rot_dim on stay as they are.  With its axis (0 .. n_axes - 1) the pair turns
+ * by the angle positions[axis][token] * inv_freq[f], formed in binary64, whose
+ * cosine and sine are each rounded to binary32 once:
+ *   c = RN32(cos), s = RN32(sin),
+ *   y_a = RN(RN(x_a c) - RN(x_b s)), y_b = RN(RN(x_b c) + RN(x_a s)).
+ * (cos and sin by Cody-Waite reduction with two parts of pi/2 and their Taylor
+ * sums, in binary64 fma; |angle| below 2^31.)
+ */
+typedef struct quarot_rotary {
+    const int32_t *positions; /* [n_axes, pos_stride] on the device, any value; NULL (paged calls
+                                 only, n_axes 1): each token's position in its sequence */
+    int64_t pos_stride;       /* elements between axes, at least T */
+    const float *inv_freq;    /* [rot_dim / 2] on the device; NULL: no rotary positions */
+    const uint8_t *axis_map;  /* HOST [rot_dim / 2], the axis of each pair; NULL: all axis 0 */
+    int32_t n_axes;           /* 1 .. 4 (text 1; time, height and width 3) */
+    int32_t rot_dim;          /* a multiple of 16, at most head_dim */
+    int32_t interleaved;
+} quarot_rotary;
+
+/*
+ * The cache of one layer.  Position t of sequence b is slot t % page_size of
+ * page page_table[b][t / page_size]; a page is [n_kv_heads, page_size, ...], so
+ * dense caches [batch, n_kv_heads, s_max, ...] are pools of one page each.
+ *   *_codes uint8 [n_pages, n_kv_heads, page_size, head_dim / 2],
+ *   *_scale, *_zero fp16 [n_pages, n_kv_heads, page_size, head_dim / group]
+ *   (formats of quarot_kv_quant),
+ *   page_table int32 [batch, max_pages], seq_lens int32 [batch],
+ *   cu_new int32 [batch + 1], non-decreasing, 0 <= cu_new <= T, all on the
+ *   device and read when the kernels run.
+ * seq_lens[b] counts the cached tokens with the new ones: new token i of n sits
+ * at position seq_lens[b] - n + i.  Entries of page_table outside 0 ..
+ * n_pages - 1 are no page: nothing is stored there and nothing seen (pages that
+ * a window has left can be given back).  Sequences may share pages that they
+ * only read.  head_dim 64, 128 or 256; group a power of two, 32 <= group <=
+ * head_dim; page_size a multiple of 16, page_size * max_pages at most 2^30.
+ */
+typedef struct quarot_paged_kv {
+    uint8_t *k_codes;
+    quarot_f16 *k_scale, *k_zero;
+    uint8_t *v_codes;
+    quarot_f16 *v_scale, *v_zero;
+    const int32_t *page_table, *seq_lens, *cu_new;
+    int64_t batch, n_kv_heads, head_dim, group, n_pages, page_size, max_pages;
+} quarot_paged_kv;
+
+/*
+ * Rotary positions of T tokens of n_heads heads, then with rotate != 0 the
+ * head's Hadamard H_head_dim / sqrt(head_dim) of the binary32 result, then
+ * RN16: what queries need before quarot_kv_paged_attention.
+ *   x fp16: head h of token t at x + t * x_stride + h * head_dim (elements);
+ *   y alike with y_stride.  Strides multiples of 8, at least n_heads * head_dim
+ *   (a slice of a fused projection's output is taken as it stands).
+ *   x == y with equal strides (in place) is allowed, other overlap is not.
+ * rotary->inv_freq and ->positions required.  head_dim 64, 128 or 256; T >= 0 (0 is
+ * a no-op).  One launch.
+ */
+quarot_status quarot_rope(const quarot_f16 *x, int64_t x_stride, quarot_f16 *y, int64_t y_stride,
+                          const quarot_rotary *rotary, int64_t T, int64_t n_heads,
+                          int64_t head_dim, int rotate, void *stream);
+
+/*
+ * The new tokens' keys and values into the pages, and their queries made ready,
+ * in one launch: keys take the rotary positions, with rotate_k the Hadamard,
+ * and quarot_kv_quant's codes, scale and zero (no fp16 in between); values the
+ * same without positions, with rotate_v the Hadamard (0 where it is fused into
+ * W_v, §4 Stage 1d); queries as quarot_rope with rotate = rotate_k.
+ *   k, v fp16 [T, n_kv_heads, head_dim], q and q_out [T, n_heads, head_dim]
+ *   with strides between tokens as in quarot_rope; q NULL with n_heads 0: no
+ *   queries; q == q_out with equal strides is allowed.
+ * rotary NULL or rotary->inv_freq NULL: no rotary positions.  Only the new
+ * tokens' slots are written.  New tokens of two sequences must not fall on the
+ * same slot.  A token whose position is negative, past the table or on no page
+ * is not stored; its query is still made ready.  T >= 0 (0 is a no-op).
+ */
+quarot_status quarot_kv_append_paged(const quarot_f16 *q, int64_t q_stride, quarot_f16 *q_out,
+                                     int64_t q_out_stride, const quarot_f16 *k, int64_t k_stride,
+                                     const quarot_f16 *v, int64_t v_stride,
+                                     const quarot_paged_kv *cache, const quarot_rotary *rotary,
+                                     int64_t T, int64_t n_heads, int rotate_k, int rotate_v,
+                                     float clip_ratio, void *stream);
+
+/*
+ * Bytes of device workspace quarot_kv_paged_attention needs (0: none).
+ * Host-only; 0 for invalid sizes.
+ */
+size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_t n_heads,
+                                                int64_t n_kv_heads, int64_t head_dim,
+                                                int64_t max_seq_len, int64_t window,
+                                                int64_t n_sinks);
+
+/*
+ * Attention of the new tokens over the pages (§4 Stage 2c with App. A.10's
+ * cache; prompts, chunks of prompts and single tokens in one call).  The query
+ * at position p sees the cached tokens t <= p with
+ *   window == 0  or  t > p - window  or  t < n_sinks,
+ * and out = RN16(softmax_t(sm_scale * q . khat_t) . vhat), khat and vhat the
+ * dequantized rows (rounded to fp16 where a kernel multiplies them as such),
+ * weights rounded to fp16 for their product, sums and softmax in binary32; a
+ * query that sees nothing gives zeros.  Codes that no query sees (slots past a
+ * sequence, pages before its window) have no influence, whatever their scales
+ * hold.
+ *   q fp16, head h of token t at q + t * q_stride + h * head_dim; query head h
+ *   reads cache head h / (n_heads / n_kv_heads); out alike with out_stride,
+ *   not overlapping q.  Rows of no sequence are not written.
+ * n_heads a multiple of n_kv_heads; window >= 0, n_sinks >= 0; sm_scale > 0;
+ * max_seq_len >= 1: the longest seq_lens to plan for (a longer one is right as
+ * well, only slower).  workspace: quarot_kv_paged_attention_workspace_size
+ * bytes, 16-byte aligned, may be NULL when that is 0; every call writes what it
+ * reads of it.  One or two launches.
+ */
+quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, quarot_f16 *out,
+                                        int64_t out_stride, const quarot_paged_kv *cache, int64_t T,
+                                        int64_t n_heads, int64_t max_seq_len, int64_t window,
+                                        int64_t n_sinks, float sm_scale, void *workspace,
+                                        size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -57,6 +57,10 @@ _SIGS = {
     "orc_gemm_i32": (_I, [_P, _P, _P, _I64, _I64, _I64]),
     "orc_dequant": (_I, [_P, _P, _P, _P, _I64, _I64]),
     "orc_linear": (_I, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _I, _F]),
+    "orc_cos_sin": (None, [ctypes.c_double, _P, _P]),
+    "orc_rope": (_I, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I]),
+    "orc_kv_quant_f32": (_I, [_P, _P, _P, _P, _I64, _I64, _I64, _F]),
+    "orc_paged_attention": (_I, [_P] * 11 + [_I64] * 10 + [ctypes.c_double]),
     "orc_kv_quant": (_I, [_P, _P, _P, _P, _I64, _I64, _I64, _I, _F]),
     "orc_kv_dequant": (_I, [_P, _P, _P, _P, _I64, _I64, _I64, _I]),
     "orc_silu_f32": (_F, [_F]),
@@ -394,6 +398,97 @@ def kv_attention(q: np.ndarray, k: tuple, v: tuple, seq_len: int, group: int = 1
                                   _ptr(vc), _ptr(_u16(vs)), _ptr(_u16(vz)), _ptr(out), nq, nkv,
                                   s_max, seq_len, D, group, float(sm_scale)), "kv_attention")
     return out.view(np.float16)
+
+
+# -- rotary positions and the paged cache ------------------------------------
+
+def cos_sin(angle: float):
+    """(cos, sin) of a binary64 angle, each rounded to binary32 once."""
+    c, s = ctypes.c_float(), ctypes.c_float()
+    lib().orc_cos_sin(float(angle), ctypes.byref(c), ctypes.byref(s))
+    return np.float32(c.value), np.float32(s.value)
+
+
+def rope(x: np.ndarray, positions: np.ndarray, inv_freq: np.ndarray, axis=None,
+         interleaved: bool = False) -> np.ndarray:
+    """x fp16 [T, H, D], positions int32 [axes, T], the axis of each pair ->
+    binary32 [T, H, D]."""
+    x = _f16(x)
+    T, H, D = x.shape
+    pos = np.ascontiguousarray(np.atleast_2d(positions), np.int32)
+    freq = np.ascontiguousarray(inv_freq, np.float32)
+    axis = np.zeros(freq.size, np.uint8) if axis is None else np.ascontiguousarray(axis, np.uint8)
+    assert pos.shape[1] == T and axis.size == freq.size and axis.max(initial=0) < pos.shape[0]
+    y = np.empty((T, H, D), np.float32)
+    _check(lib().orc_rope(_ptr(_u16(x)), _ptr(y), _ptr(pos), _ptr(freq), _ptr(axis), T, H, D,
+                          freq.size, int(interleaved)), "rope")
+    return y
+
+
+def rotate_rows(y: np.ndarray) -> np.ndarray:
+    """The head's Hadamard of binary32 rows [..., D], binary32."""
+    return rotate_f32(y.reshape(-1, y.shape[-1])).reshape(y.shape)
+
+
+def kv_quant_f32(y: np.ndarray, group: int = 128, clip: float = 0.95):
+    """Binary32 rows [rows, D] -> (codes, scale, zero) as kv_quant."""
+    y = np.ascontiguousarray(y, np.float32)
+    rows, D = y.shape
+    q = np.empty((rows, D // 2), np.uint8)
+    sc = np.empty((rows, D // group), np.uint16)
+    ze = np.empty((rows, D // group), np.uint16)
+    _check(lib().orc_kv_quant_f32(_ptr(y), _ptr(q), _ptr(sc), _ptr(ze), rows, D, group, clip),
+           "kv_quant_f32")
+    return q, sc.view(np.float16), ze.view(np.float16)
+
+
+def paged_place(table, n_pages: int, page: int, seq_lens, cu):
+    """For each new token of a batch: (row, sequence, position, page or -1,
+    slot in the page)."""
+    out = []
+    for b in range(len(seq_lens)):
+        for r in range(cu[b], cu[b + 1]):
+            t = int(seq_lens[b]) - (int(cu[b + 1]) - r)
+            pg = -1
+            if t >= 0 and t // page < table.shape[1]:
+                pg = int(table[b, t // page])
+            out.append((r, b, t, pg if 0 <= pg < n_pages else -1, t % page))
+    return out
+
+
+def kv_append_paged(x: np.ndarray, cache, table, seq_lens, cu, group: int = 128,
+                    clip: float = 0.95):
+    """Binary32 rows x [T, Hkv, D] (rotary positions and Hadamard done) into
+    copies of the pools cache = (codes [pages, Hkv, page, D/2], scale, zero)."""
+    codes, scale, zero = (np.array(c) for c in cache)
+    T, H, D = x.shape
+    q, s, z = kv_quant_f32(x.reshape(-1, D), group, clip)
+    q, s, z = (a.reshape(T, H, -1) for a in (q, s, z))
+    for r, _, _, pg, slot in paged_place(table, codes.shape[0], codes.shape[2], seq_lens, cu):
+        if pg >= 0:
+            codes[pg, :, slot], scale[pg, :, slot], zero[pg, :, slot] = q[r], s[r], z[r]
+    return codes, scale, zero
+
+
+def paged_attention(q: np.ndarray, k, v, table, seq_lens, cu, group: int = 128, window: int = 0,
+                    sinks: int = 0, sm_scale: float = None, out=None) -> np.ndarray:
+    """q fp16 [T, H, D] over pools k, v = (codes [pages, Hkv, page, D/2], scale,
+    zero) -> binary64 [T, H, D]; rows of no sequence keep what `out` holds."""
+    q = _f16(q)
+    T, H, D = q.shape
+    kc, ks, kz = (np.ascontiguousarray(k[0], np.uint8), _f16(k[1]), _f16(k[2]))
+    vc, vs, vz = (np.ascontiguousarray(v[0], np.uint8), _f16(v[1]), _f16(v[2]))
+    pages, hkv, page = kc.shape[:3]
+    table = np.ascontiguousarray(table, np.int32)
+    lens, cu = np.ascontiguousarray(seq_lens, np.int32), np.ascontiguousarray(cu, np.int32)
+    assert cu.size == lens.size + 1 == table.shape[0] + 1 and 0 <= cu[0] and cu[-1] <= T
+    out = np.zeros((T, H, D)) if out is None else np.array(out, np.float64)
+    _check(lib().orc_paged_attention(
+        _ptr(_u16(q)), _ptr(kc), _ptr(_u16(ks)), _ptr(_u16(kz)), _ptr(vc), _ptr(_u16(vs)),
+        _ptr(_u16(vz)), _ptr(table), _ptr(lens), _ptr(cu), _ptr(out), lens.size, H, hkv, D, group,
+        pages, page, table.shape[1], window, sinks,
+        D ** -0.5 if sm_scale is None else float(np.float32(sm_scale))), "paged_attention")
+    return out
 
 
 # -- prologues of the two online-Hadamard sites -----------------------------

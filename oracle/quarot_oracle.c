@@ -1288,6 +1288,149 @@ int orc_kv_attention(const uint16_t *q, const uint8_t *kc, const uint16_t *ks,
 }
 
 /* ------------------------------------------------------------------------ */
+/* Rotary positions and attention over a paged cache.                       */
+/* ------------------------------------------------------------------------ */
+
+/* cos and sin of an angle (|a| < 2^31), each rounded to binary32 once from
+ * binary64: a = k pi/2 + r with k = rint(a 2/pi) and pi/2 in two parts, then
+ * the Taylor sums of sin to r^15 and of cos to r^16 by fma. */
+void orc_cos_sin(double a, float *cos32, float *sin32)
+{
+    static const double fs[7] = {-6.0, 120.0, -5040.0, 362880.0, -39916800.0, 6227020800.0,
+                                 -1307674368000.0};  /* 3!, 5!, .. 15! with their signs */
+    static const double fc[8] = {-2.0, 24.0, -720.0, 40320.0, -3628800.0, 479001600.0,
+                                 -87178291200.0, 20922789888000.0};
+    const double k = rint(a * 0x1.45f306dc9c883p-1);
+    double r = fma(-k, 0x1.921fb54442d18p+0, a);
+    r = fma(-k, 0x1.1a62633145c07p-54, r);
+    const double x = r * r;
+    double s = 1.0 / fs[6], c = 1.0 / fc[7];
+    for (int i = 5; i >= 0; i--)
+        s = fma(s, x, 1.0 / fs[i]);
+    s = fma(s * x, r, r);
+    for (int i = 6; i >= 0; i--)
+        c = fma(c, x, 1.0 / fc[i]);
+    c = fma(c, x, 1.0);
+    const int q = (int)((int64_t)k & 3);
+    const double cv = (q & 1) ? s : c, sv = (q & 1) ? c : s;
+    *cos32 = (float)(q == 1 || q == 2 ? -cv : cv);
+    *sin32 = (float)(q >= 2 ? -sv : sv);
+}
+
+/* x fp16 [T, H, D] -> y binary32: pair f of half turned by pos[axis[f]][t] *
+ * inv_freq[f]; elements past 2 half as they are. */
+int orc_rope(const uint16_t *x, float *y, const int32_t *pos, const float *inv_freq,
+             const uint8_t *axis, int64_t T, int64_t H, int64_t D, int64_t half, int interleaved)
+{
+    if (T < 0 || H <= 0 || D <= 0 || half < 0 || 2 * half > D)
+        return ORC_ERR_ARG;
+#pragma omp parallel for schedule(static)
+    for (int64_t t = 0; t < T; t++) {
+        for (int64_t i = 0; i < H * D; i++)
+            y[t * H * D + i] = orc_f16_to_f32(x[t * H * D + i]);
+        for (int64_t f = 0; f < half; f++) {
+            float c, s;
+            orc_cos_sin((double)pos[axis[f] * T + t] * (double)inv_freq[f], &c, &s);
+            const int64_t ia = interleaved ? 2 * f : f, ib = interleaved ? 2 * f + 1 : f + half;
+            for (int64_t h = 0; h < H; h++) {
+                float *row = y + (t * H + h) * D;
+                const float a = row[ia], b = row[ib];
+                row[ia] = a * c - b * s;
+                row[ib] = b * c + a * s;
+            }
+        }
+    }
+    return ORC_OK;
+}
+
+/* orc_kv_quant without rotation of binary32 rows (zeros taken as +0). */
+int orc_kv_quant_f32(const float *y, uint8_t *q, uint16_t *scale, uint16_t *zero, int64_t rows,
+                     int64_t D, int64_t G, float clip)
+{
+    if (D <= 0 || D > 512 || (D & 1) || G <= 0 || (G & 1) || D % G || rows < 0)
+        return ORC_ERR_ARG;
+#pragma omp parallel for schedule(static)
+    for (int64_t r = 0; r < rows; r++) {
+        float t[512];
+        for (int64_t i = 0; i < D; i++)
+            t[i] = y[r * D + i] + 0.0f;
+        kv_quant_row(t, D, G, clip, q + r * (D / 2), scale + r * (D / G), zero + r * (D / G));
+    }
+    return ORC_OK;
+}
+
+/* Pool row of position t of sequence b for cache head h, or -1. */
+static int64_t paged_row(const int32_t *table, int64_t max_pages, int64_t n_pages, int64_t page,
+                         int64_t hkv, int64_t b, int64_t h, int64_t t)
+{
+    if (t < 0 || t / page >= max_pages)
+        return -1;
+    const int64_t pg = table[b * max_pages + t / page];
+    return pg < 0 || pg >= n_pages ? -1 : (pg * hkv + h) * page + t % page;
+}
+
+/* Attention of new tokens over a paged cache, all in binary64: the query of
+ * row r of sequence b (rows cu[b] .. cu[b+1] - 1) sits at position
+ * p = len[b] - (cu[b+1] - r) and sees t <= p with window == 0, t > p - window
+ * or t < sinks, on pages that exist; nothing seen gives zeros.  Rows of no
+ * sequence of out [T, H, D] are left alone. */
+int orc_paged_attention(const uint16_t *q, const uint8_t *kc, const uint16_t *ks,
+                        const uint16_t *kz, const uint8_t *vc, const uint16_t *vs,
+                        const uint16_t *vz, const int32_t *table, const int32_t *len,
+                        const int32_t *cu, double *out, int64_t B, int64_t H, int64_t hkv,
+                        int64_t D, int64_t G, int64_t n_pages, int64_t page, int64_t max_pages,
+                        int64_t window, int64_t sinks, double sm_scale)
+{
+    if (B <= 0 || H <= 0 || hkv <= 0 || H % hkv || D <= 0 || (D & 1) || G <= 0 || D % G)
+        return ORC_ERR_ARG;
+    const int64_t rep = H / hkv, ng = D / G;
+    int err = 0;
+    for (int64_t b = 0; b < B; b++)
+#pragma omp parallel for schedule(dynamic) reduction(| : err)
+        for (int64_t i = (int64_t)cu[b] * H; i < (int64_t)cu[b + 1] * H; i++) {
+            const int64_t r = i / H, h = (i % H) / rep, p = len[b] - (cu[b + 1] - r);
+            double *sc = (double *)malloc((size_t)(p >= 0 ? p + 1 : 1) * sizeof(double));
+            double *o = out + i * D, mx = -INFINITY, l = 0.0;
+            for (int64_t d = 0; d < D; d++)
+                o[d] = 0.0;
+            if (!sc) {
+                err |= 1;
+                continue;
+            }
+            for (int pass = 0; pass < 2; pass++)
+                for (int64_t t = 0; t <= p; t++) {
+                    if (window > 0 && t <= p - window && t >= sinks)
+                        continue;
+                    const int64_t row = paged_row(table, max_pages, n_pages, page, hkv, b, h, t);
+                    if (row < 0)
+                        continue;
+                    const uint8_t *c = (pass ? vc : kc) + row * (D / 2);
+                    const uint16_t *s = (pass ? vs : ks) + row * ng, *z = (pass ? vz : kz) + row * ng;
+                    const double w = pass ? exp(sc[t] - mx) : 0.0;
+                    double acc = 0.0;
+                    l += w;
+                    for (int64_t d = 0; d < D; d++) {
+                        const double val = (double)((c[d / 2] >> ((d & 1) * 4)) & 0xF) *
+                                               orc_f16_to_f32(s[d / G]) + orc_f16_to_f32(z[d / G]);
+                        if (pass)
+                            o[d] += w * val;
+                        else
+                            acc += (double)orc_f16_to_f32(q[i * D + d]) * val;
+                    }
+                    if (!pass) {
+                        sc[t] = acc * sm_scale;
+                        if (sc[t] > mx)
+                            mx = sc[t];
+                    }
+                }
+            for (int64_t d = 0; d < D; d++)
+                o[d] = l > 0.0 ? o[d] / l : 0.0;
+            free(sc);
+        }
+    return err ? ORC_ERR_NOMEM : ORC_OK;
+}
+
+/* ------------------------------------------------------------------------ */
 /* Threads (for timing the oracle as a CPU baseline).                       */
 /* ------------------------------------------------------------------------ */
 

@@ -38,6 +38,21 @@ _I64 = ctypes.c_int64
 _I = ctypes.c_int
 _F = ctypes.c_float
 
+class _Rotary(ctypes.Structure):
+    """quarot_rotary of include/quarot.h."""
+    _fields_ = [("positions", _P), ("pos_stride", _I64), ("inv_freq", _P), ("axis_map", _P),
+                ("n_axes", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class _PagedKV(ctypes.Structure):
+    """quarot_paged_kv of include/quarot.h."""
+    _fields_ = [(n, _P) for n in ("k_codes", "k_scale", "k_zero", "v_codes", "v_scale", "v_zero",
+                                  "page_table", "seq_lens", "cu_new")] + \
+        [(n, _I64) for n in ("batch", "n_kv_heads", "head_dim", "group", "n_pages", "page_size",
+                             "max_pages")]
+
+
 # name -> (restype, argtypes), exactly the declarations of include/quarot.h
 SIGNATURES = {
     "quarot_status_string": (ctypes.c_char_p, [_I]),
@@ -84,6 +99,12 @@ SIGNATURES = {
     "quarot_kv_attention_workspace_size": (ctypes.c_size_t, [_I64, _I64, _I64]),
     "quarot_kv_decode_attention": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I64,
                                         _I64, _I64, _F, _P, ctypes.c_size_t, _P]),
+    "quarot_rope": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I, _P]),
+    "quarot_kv_append_paged": (_I, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _I64, _I64,
+                                    _I, _I, _F, _P]),
+    "quarot_kv_paged_attention_workspace_size": (ctypes.c_size_t, [_I64] * 8),
+    "quarot_kv_paged_attention": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _F,
+                                       _P, ctypes.c_size_t, _P]),
 }
 
 # name -> (restype, argtypes), exactly the declarations of include/quarot_probe.h
@@ -866,6 +887,236 @@ def quarot_kv_decode_attention(q: torch.Tensor, k_cache, v_cache, seq_len: int,
     return out
 
 
+# -- rotary positions and the paged KV cache ----------------------------------
+#
+# Token rows [T, heads, D] may be slices of a wider tensor (the queries, keys
+# and values of one projection's output): the heads of a token follow one
+# another, the tokens may lie further apart.
+
+def _half_rows(t: torch.Tensor, name: str):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.float16:
+        raise TypeError(f"{name} must be {torch.float16}, got {t.dtype}")
+    _ndim(t, 3, name)
+
+
+def _token_rows(t: torch.Tensor, name: str):
+    """(address, elements between tokens) of fp16 [T, heads, D]."""
+    _half_rows(t, name)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    T, H, D = t.shape
+    st = t.stride()
+    if (D > 1 and st[2] != 1) or (H > 1 and st[1] != D):
+        raise ValueError(f"{name}: the heads of a token must follow one another, got strides {st}")
+    return t.data_ptr(), st[0] if T > 1 else H * D
+
+
+def _on_device(dev, **tensors):
+    """Every tensor on `dev`, and `dev` the current device (whose stream the
+    call runs on)."""
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}, got {t.device}")
+
+
+def _sections(sections, half: int):
+    """The axis of each of `half` pairs as a host array, and the axes: runs of
+    the given lengths for axis 0, 1, .. (a list of ints), or the axis of each
+    pair itself (a sequence of `half` axes given as bytes)."""
+    if sections is None:
+        return None, 1
+    if isinstance(sections, (bytes, bytearray)):
+        axes = bytes(sections)
+        n = max(axes, default=0) + 1
+    else:
+        sections = [int(x) for x in sections]
+        if any(x < 0 for x in sections) or not 1 <= len(sections) <= 4:
+            raise ValueError(f"sections must be the pairs of 1 to 4 axes, got {sections}")
+        axes = b"".join(bytes([a]) * x for a, x in enumerate(sections))
+        n = len(sections)
+    if len(axes) != half:
+        raise ValueError(f"sections must cover the {half} pairs, got {len(axes)}")
+    return axes, n
+
+
+def _rotary(positions, inv_freq, sections, interleaved: bool, T: int, D: int):
+    """The quarot_rotary of a call, and the host array that it points to."""
+    _ndim(inv_freq, 1, "inv_freq")
+    half = inv_freq.shape[0]
+    if 2 * half > D:
+        raise ValueError(f"inv_freq must hold at most {D // 2} elements, got {half}")
+    axes, n = _sections(sections, half)
+    stride = T
+    if positions is not None:
+        if positions.dim() == 1:
+            positions = positions[None]
+        _ndim(positions, 2, "positions")
+        if positions.shape[0] < n or positions.shape[1] < T:
+            raise ValueError(f"positions must have shape {(n, T)}, got {tuple(positions.shape)}")
+        n = positions.shape[0]
+        if positions.dtype != torch.int32:
+            raise TypeError(f"positions must be {torch.int32}, got {positions.dtype}")
+        if not positions.is_cuda:
+            raise ValueError("positions must be a device tensor")
+        if T > 1 and positions.stride(1) != 1:
+            raise ValueError("positions must be contiguous along the tokens")
+        if n > 1:
+            stride = positions.stride(0)
+    host = (ctypes.c_uint8 * half)(*axes) if axes is not None else None
+    r = _Rotary(positions.data_ptr() if positions is not None else None, stride,
+                _ptr(inv_freq, torch.float32, "inv_freq"),
+                ctypes.cast(host, _P) if host is not None else None, n, 2 * half,
+                int(bool(interleaved)))
+    return r, host
+
+
+def _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group: int, rows: torch.Tensor,
+              name: str, kv_rows: bool):
+    """The quarot_paged_kv of a call on `rows` [T, heads, D]; caches are (codes
+    [n_pages, n_kv_heads, page_size, D/2], scale, zero [n_pages, n_kv_heads,
+    page_size, D/group])."""
+    kc, ks, kz = k_cache
+    vc, vs, vz = v_cache
+    _ndim(kc, 4, "k_codes")
+    pages, heads, page, half = kc.shape
+    _group(group, 2 * half)
+    _shape(vc, kc.shape, "v_codes")
+    consts = (pages, heads, page, 2 * half // group)
+    for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
+        _shape(t, consts, nm)
+    _ndim(page_table, 2, "page_table")
+    B, most = page_table.shape
+    _shape(seq_lens, (B,), "seq_lens")
+    _shape(cu_new, (B + 1,), "cu_new")
+    _shape(rows, (rows.shape[0], heads if kv_rows else rows.shape[1], 2 * half), name)
+    _on_device(kc.device, k_scale=ks, k_zero=kz, v_codes=vc, v_scale=vs, v_zero=vz,
+               page_table=page_table, seq_lens=seq_lens, cu_new=cu_new)
+    f16, i32 = torch.float16, torch.int32
+    return _PagedKV(
+        _ptr(kc, torch.uint8, "k_codes"), _ptr(ks, f16, "k_scale"), _ptr(kz, f16, "k_zero"),
+        _ptr(vc, torch.uint8, "v_codes"), _ptr(vs, f16, "v_scale"), _ptr(vz, f16, "v_zero"),
+        _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"),
+        _ptr(cu_new, i32, "cu_new"), B, heads, 2 * half, group, pages, page, most)
+
+
+def quarot_rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, sections=None,
+                interleaved: bool = False, rotate: bool = False,
+                y: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Rotary positions of x fp16 [T, heads, D], then with rotate the head's
+    Hadamard.  positions int32 [T], or [axes, T] with sections (how many of the
+    len(inv_freq) pairs each axis takes, in order; or the axis of each pair as
+    bytes); inv_freq float32 [rot_dim / 2]."""
+    _half_rows(x, "x")
+    _shape(y, x.shape, "y")
+    T, H, D = x.shape
+    r, host = _rotary(positions, inv_freq, sections, interleaved, T, D)
+    _on_device(x.device, positions=positions, inv_freq=inv_freq, y=y)
+    if y is None:
+        y = torch.empty((T, H, D), dtype=torch.float16, device=x.device)
+    (xp, xs), (yp, ys) = _token_rows(x, "x"), _token_rows(y, "y")
+    _check("quarot_rope", lib().quarot_rope(
+        xp, xs, yp, ys, ctypes.byref(r), T, H, D, int(bool(rotate)), _stream(stream)))
+    return y
+
+
+def quarot_kv_append_paged(k: torch.Tensor, v: torch.Tensor, k_cache, v_cache,
+                           page_table: torch.Tensor, seq_lens: torch.Tensor,
+                           cu_new: torch.Tensor, group: int = 128,
+                           q: Optional[torch.Tensor] = None,
+                           positions: Optional[torch.Tensor] = None,
+                           inv_freq: Optional[torch.Tensor] = None, sections=None,
+                           interleaved: bool = False, rotate_k: bool = True,
+                           rotate_v: bool = False, clip_ratio: float = 0.95,
+                           q_out: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None):
+    """The new tokens' keys and values k, v fp16 [T, n_kv_heads, D] into the
+    pages (rotary positions where inv_freq is given, Hadamard, 4-bit codes), and
+    their queries q [T, n_heads, D] made ready for quarot_kv_paged_attention.
+    positions None: each token's position in its sequence.  Returns the queries
+    (rows of no sequence unwritten), or None without q."""
+    _half_rows(k, "k")
+    T, Hkv, D = k.shape
+    _shape(v, k.shape, "v")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    H = 0
+    if q is not None:
+        _half_rows(q, "q")
+        H = q.shape[1]
+        _shape(q, (T, H, D), "q")
+        _shape(q_out, (T, H, D), "q_out")
+    if inv_freq is None and (positions is not None or sections is not None):
+        raise ValueError("positions and sections need inv_freq")
+    cache = _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group, k, "k", True)
+    r = None
+    if inv_freq is not None:
+        r, host = _rotary(positions, inv_freq, sections, interleaved, T, D)
+    _on_device(k_cache[0].device, k=k, v=v, q=q, q_out=q_out, positions=positions,
+               inv_freq=inv_freq)
+    if q is not None and q_out is None:
+        q_out = torch.empty((T, H, D), dtype=torch.float16, device=q.device)
+    qp = qs = op = os_ = None
+    if q is not None:
+        (qp, qs), (op, os_) = _token_rows(q, "q"), _token_rows(q_out, "q_out")
+    (kp, kst), (vp, vst) = _token_rows(k, "k"), _token_rows(v, "v")
+    _check("quarot_kv_append_paged", lib().quarot_kv_append_paged(
+        qp, qs or 0, op, os_ or 0, kp, kst, vp, vst, ctypes.byref(cache),
+        ctypes.byref(r) if r is not None else None, T, H, int(bool(rotate_k)),
+        int(bool(rotate_v)), float(clip_ratio), _stream(stream)))
+    return q_out
+
+
+def quarot_kv_paged_attention_workspace_size(T: int, batch: int, n_heads: int, n_kv_heads: int,
+                                             head_dim: int, max_seq_len: int, window: int = 0,
+                                             n_sinks: int = 0) -> int:
+    return int(lib().quarot_kv_paged_attention_workspace_size(
+        T, batch, n_heads, n_kv_heads, head_dim, max_seq_len, window, n_sinks))
+
+
+def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: torch.Tensor,
+                              seq_lens: torch.Tensor, cu_new: torch.Tensor, group: int = 128,
+                              window: int = 0, n_sinks: int = 0,
+                              max_seq_len: Optional[int] = None,
+                              sm_scale: Optional[float] = None,
+                              out: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None,
+                              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries q fp16 [T, n_heads, D] (as
+    quarot_kv_append_paged returns them) over the pages: causal, with a sliding
+    window and sinks where window > 0.  max_seq_len: the longest sequence to
+    plan for (default: what the table holds).  Returns fp16 [T, n_heads, D];
+    rows of no sequence are not written."""
+    _half_rows(q, "q")
+    T, H, D = q.shape
+    _shape(out, q.shape, "out")
+    cache = _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group, q, "q", False)
+    _on_device(k_cache[0].device, q=q, out=out, workspace=workspace)
+    if max_seq_len is None:
+        max_seq_len = cache.max_pages * cache.page_size
+    if sm_scale is None:
+        sm_scale = D ** -0.5
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.float16, device=q.device)
+    (qp, qs), (op, ost) = _token_rows(q, "q"), _token_rows(out, "out")
+    if workspace is None:
+        need = quarot_kv_paged_attention_workspace_size(
+            T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check("quarot_kv_paged_attention", lib().quarot_kv_paged_attention(
+        qp, qs, op, ost, ctypes.byref(cache), T, H, int(max_seq_len), int(window), int(n_sinks),
+        float(sm_scale),
+        _ptr(workspace, torch.uint8, "workspace") if workspace is not None else None,
+        workspace.numel() if workspace is not None else 0, _stream(stream)))
+    return out
+
+
 __all__ = [
     "QuarotError", "lib", "probe_lib", "quarot_version", "quarot_device_peaks", "quarot_mfma_probe",
     "quarot_hadamard_factor",
@@ -880,4 +1131,6 @@ __all__ = [
     "quarot_mfma_probe_fp6", "quarot_pack_e3m2", "quarot_w4a4_gemm_e3m2",
     "quarot_quant_int4_e3m2", "quarot_linear_e3m2_workspace_size", "quarot_linear_e3m2",
     "quarot_swiglu_quant_e3m2", "prepare_weight_e3m2", "quarot_linear_e3m2_scratch",
+    "quarot_rope", "quarot_kv_append_paged", "quarot_kv_paged_attention_workspace_size",
+    "quarot_kv_paged_attention",
 ]

@@ -7,7 +7,7 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "common.hpp"
+#include "capi_util.hpp"
 #include "hadamard_factors.hpp"
 
 using namespace quarot;
@@ -17,11 +17,6 @@ namespace {
 thread_local int g_last_hip_error = 0;
 
 constexpr int kMaxN = 32768;
-
-bool aligned16(const void *p)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
 
 // n = 2^k * m with m picked by the odd part of n.
 bool factor(int64_t n, int *k, int *m)
@@ -45,23 +40,6 @@ bool factor(int64_t n, int *k, int *m)
     return false;
 }
 
-// RN32(1/sqrt(n)), through double (exact square root, one division).
-float rotation_scale(int64_t n)
-{
-    return (float)(1.0 / std::sqrt((double)n));
-}
-
-bool clip_ok(float c)
-{
-    return c > 0.0f && c <= 1.0f;
-}
-
-quarot_status hip_fail(hipError_t e)
-{
-    g_last_hip_error = (int)e;
-    return QUAROT_ERR_HIP;
-}
-
 // Failure injection for tests of the error path: when the environment
 // variable QUAROT_FAKE_HIP_ERROR holds the name of an entry point, that
 // entry point behaves as if its first HIP runtime call had failed with
@@ -77,6 +55,16 @@ bool fake_hip_error(const char *call)
 
 // The device this thread's last check accepted and its compute units.
 thread_local int ok_dev = -1, ok_cus = 256;
+
+}  // namespace
+
+namespace quarot {
+
+quarot_status hip_fail(hipError_t e)
+{
+    g_last_hip_error = (int)e;
+    return QUAROT_ERR_HIP;
+}
 
 // The device of the calling thread must be a gfx950.  Cached per thread
 // and device (a host-side query, no device work).  `call` names the entry
@@ -105,6 +93,10 @@ quarot_status check_device(const char *call)
     ok_dev = dev;
     return QUAROT_OK;
 }
+
+}  // namespace quarot
+
+namespace {
 
 quarot_status check_rot_size(int64_t n, bool rotate, int epi, int *k, int *m)
 {

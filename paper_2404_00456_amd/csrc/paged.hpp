@@ -1,0 +1,91 @@
+// The paged 4-bit KV cache: what its kernels and their launchers share.
+//
+// A batch holds the new tokens of B sequences one after the other: rows
+// cu[b] .. cu[b + 1] - 1 of T belong to sequence b, whose cache holds len[b]
+// tokens with the new ones, so new token i of n sits at position
+// len - n + i.  Position t of sequence b is slot t % page of page
+// table[b][t / page] of the pools.  All of cu, len and table live on the
+// device: kernels bound what they read from them (a page outside the pool is
+// no page, a row outside 0 .. T is no row), so that no content of theirs
+// leads outside a buffer.
+#pragma once
+
+#include "common.hpp"
+#include "paged_plan.hpp"
+
+namespace quarot {
+
+constexpr int APPEND_THREADS = 256;  // of a block of the append kernel
+
+// One pool: codes [pages, heads, page, D/2], scale and zero
+// [pages, heads, page, D/G].
+struct PagedPool {
+    uint8_t *c;
+    uint16_t *s, *z;
+};
+
+struct PagedMap {
+    const int32_t *table;  // [B, max_pages]
+    const int32_t *len;    // [B]
+    const int32_t *cu;     // [B + 1]
+    int T, B;
+    int max_pages, n_pages, page;
+    paged::Divisor div;    // by page
+};
+
+struct RopeArgs {
+    const int32_t *pos;     // [axes, pos_stride], or null: the cache position
+    int64_t pos_stride;
+    const float *inv_freq;  // [half], or null: no rotary
+    int half;               // pairs of a head row
+    int interleaved;        // pairs (2f, 2f + 1) instead of (f, f + half)
+    uint32_t axis[8];       // axis of pair f: bits 2 (f % 16) .. + 1 of word f / 16
+};
+
+struct AppendArgs {
+    const uint16_t *q, *k, *v;  // rows of T tokens; k, v null for the rotary alone
+    int64_t q_stride, k_stride, v_stride;  // elements between tokens
+    uint16_t *qo;
+    int64_t qo_stride;
+    PagedPool kp, vp;
+    PagedMap map;
+    RopeArgs rope;
+    int hq, hkv;
+    int D, G;
+    int rot_k, rot_v;  // Hadamard of the queries and keys, of the values
+    float c;           // RN32(1 / sqrt(D))
+    float clip;
+};
+
+struct PagedAttnArgs {
+    const uint16_t *q;
+    int64_t q_stride;
+    uint16_t *out;
+    int64_t out_stride;
+    PagedPool kp, vp;
+    PagedMap map;
+    int hq, hkv, rep;
+    int D, G;
+    int window, sinks;  // window 0: none
+    float sm_scale;
+    int splits;
+    float *part_o;      // [T * hq, splits, D]
+    float *part_ml;     // [T * hq, splits, 2]: maximum (in log2 units), sum
+};
+
+// Row (head 0) of position t of sequence b in the pools, or -1: no page.
+__device__ __forceinline__ int64_t pool_row(const PagedMap &m, int hkv, int b, int t)
+{
+    const int pi = (int)(__umulhi((uint32_t)t, m.div.mul) >> m.div.sh);
+    if (t < 0 || pi >= m.max_pages)
+        return -1;
+    const int page = m.table[(int64_t)b * m.max_pages + pi];
+    if (page < 0 || page >= m.n_pages)
+        return -1;
+    return (int64_t)page * hkv * m.page + (t - pi * m.page);
+}
+
+hipError_t launch_append(const AppendArgs &a, hipStream_t s);
+hipError_t launch_paged_attention(const PagedAttnArgs &a, const paged::Plan &p, hipStream_t s);
+
+}  // namespace quarot

@@ -1,0 +1,502 @@
+// Attention of new tokens over the paged 4-bit KV cache, for gfx950.
+//
+// Query i of sequence b sits at position p = len - n + i and sees the cached
+// tokens t <= p with t > p - window (where there is a window) or t < sinks:
+//   out = softmax_t(sm_scale q . khat_t) . vhat,  khat = code * scale + zero,
+// and zero where it sees nothing.  The query heads of one cache head are rows
+// of the same tile, so that a cached token is unpacked once for all of them:
+// row r of a sequence is its new token r / rep, head r % rep.
+//
+// k_paged_tile: a block takes 32 rows per wave and walks over the tokens that
+// any of them sees, 64 at a time.  The codes of a step become fp16 values in
+// LDS (RN16 of code * scale + zero, one rounding, as quarot_kv_dequant gives
+// them; half an fp16 step of a key or value is what the fp16 output keeps of
+// it as well).  Scores are taken transposed, S = K Q^T, so that the lane that
+// holds a query's scores also holds its share of the weights as the B operand
+// of O = V^T P^T: the weights never leave their registers.  Softmax sums and
+// outputs are binary32; weights are rounded to fp16 for the product.
+#include <algorithm>
+
+#include "paged.hpp"
+
+namespace quarot {
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr int TT = paged::STEP;
+
+// What a block of MR query rows works on.
+struct Work : paged::Span {
+    int b;     // sequence
+    int tok0;  // first batch row (new token) of the sequence
+};
+
+template <int MR>
+__device__ __forceinline__ Work find_work(const PagedAttnArgs &a, int slot, int *sh)
+{
+    const PagedMap &m = a.map;
+    if (threadIdx.x == 0)
+        *sh = -1;
+    __syncthreads();
+    for (int b = threadIdx.x; b < m.B; b += blockDim.x)
+        if (paged::first_slot((int64_t)m.cu[b] * a.rep, b, MR) <= slot &&
+            slot < paged::first_slot((int64_t)m.cu[b + 1] * a.rep, b + 1, MR))
+            *sh = b;
+    __syncthreads();
+    Work w = {};
+    w.b = __builtin_amdgcn_readfirstlane(*sh);
+    if (w.b < 0)
+        return w;
+    const int c0 = m.cu[w.b], c1 = m.cu[w.b + 1];
+    static_cast<paged::Span &>(w) =
+        paged::span(c0, c1, m.len[w.b], m.T, m.max_pages * m.page, a.rep,
+                    slot - paged::first_slot((int64_t)c0 * a.rep, w.b, MR), MR, a.window, a.sinks,
+                    a.splits);
+    w.tok0 = c0;
+    return w;
+}
+
+__device__ __forceinline__ h2v bits_h2(uint32_t b)
+{
+    return __builtin_bit_cast(h2v, b);
+}
+
+// Two codes as fp16 integers: or-ed into the significand of 1024 (where fp16
+// values are spaced by 1) or, for the nibbles at bits 4-7 and 20-23, of 64
+// (spaced by 1/16), minus that.
+template <bool HI>
+__device__ __forceinline__ h2v nib_pair(uint32_t w)
+{
+    const uint32_t x = HI ? (w & 0x00F000F0u) | 0x54005400u : (w & 0x000F000Fu) | 0x64006400u;
+    const _Float16 b = HI ? (_Float16)-64.0f : (_Float16)-1024.0f;
+    const h2v off = {b, b};
+    return bits_h2(x) + off;
+}
+
+__device__ __forceinline__ h2v fma2(h2v a, h2v b, h2v c)
+{
+    return __builtin_elementwise_fma(a, b, c);
+}
+
+// 16 bytes of 8 fp16 elements in the order 0, 4, 1, 5, 2, 6, 3, 7, in which
+// the nibble pairs of a dword of codes come out
+__device__ __forceinline__ uint4 nib_order(uint4 r)
+{
+    return make_uint4(perm_b32(r.z, r.x, 0x05040100u), perm_b32(r.z, r.x, 0x07060302u),
+                      perm_b32(r.w, r.y, 0x05040100u), perm_b32(r.w, r.y, 0x07060302u));
+}
+
+// The values of a dword of codes (8 elements) in that order.
+__device__ __forceinline__ uint4 unpack8(uint32_t w, h2v s, h2v z)
+{
+    const uint32_t w8 = w >> 8;
+    return make_uint4(__builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w8), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w8), s, z)));
+}
+
+__device__ __forceinline__ h2v pair_of(uint32_t lo, uint32_t hi)
+{
+    return bits_h2(lo | (hi << 16));
+}
+
+// Token block i of a step: K as fp16 rows [64][D], the 16-byte unit u of row t
+// at u ^ (t & swizzle); V transposed, [D][64] with the tokens of a 16-token
+// group in the order that the scores' registers have (4 h + r, then 8 + 4 h +
+// r, for lane half h), the 16-byte unit u of dimension d at u ^ ((d ^ d / 8) &
+// 7).  Both swizzles spread the writes and the reads over the banks.
+template <int D>
+struct Stage {
+    static constexpr int K_BYTES = TT * D * 2, V_BYTES = TT * D * 2;
+    static constexpr int KSW = D == 64 ? 7 : 15;
+    uint8_t k[K_BYTES];
+    uint8_t v[V_BYTES];
+    int ok[4];  // the page of each 16-token group exists
+};
+
+// What a thread reads of a step ahead of its use.  Items 0 .. 2 D - 1 are 32
+// elements of a key, items 2 D .. 4 D - 1 8 elements of 4 tokens' values.
+template <int D, int NT>
+struct Ahead {
+    static constexpr int ITEMS = 4 * D;
+    static constexpr int N = (ITEMS + NT - 1) / NT;
+    uint4 c[N];       // codes: a key's 32, or 8 of each of 4 tokens
+    uint32_t sc[N][4];  // key: scale, zero; values: scale pairs, zero pairs
+    int ok[N];
+};
+
+template <int D, int NT>
+__device__ __forceinline__ void read_ahead(const PagedAttnArgs &a, const Work &w, int h, int t0,
+                                           Ahead<D, NT> &r)
+{
+    using A = Ahead<D, NT>;
+    const int ng = D / a.G;
+#pragma unroll
+    for (int i = 0; i < A::N; ++i) {
+        const int item = threadIdx.x + i * NT;
+        r.ok[i] = 0;
+        r.c[i] = make_uint4(0, 0, 0, 0);
+        r.sc[i][0] = r.sc[i][1] = r.sc[i][2] = r.sc[i][3] = 0;
+        if (item < 2 * D) {
+            const int t = t0 + item / (D / 32), sl = item % (D / 32);
+            int64_t row = pool_row(a.map, a.hkv, w.b, t);
+            if (row >= 0) {
+                row += (int64_t)h * a.map.page;
+                r.ok[i] = 1;
+                r.c[i] = *reinterpret_cast<const uint4 *>(a.kp.c + row * (D / 2) + sl * 16);
+                const int64_t g = row * ng + sl * 32 / a.G;
+                r.sc[i][0] = a.kp.s[g];
+                r.sc[i][1] = a.kp.z[g];
+            }
+        } else if (item < 4 * D) {
+            const int j = item - 2 * D;
+            const int t = t0 + j / (D / 8) * 4, dg = j % (D / 8);
+            int64_t row = pool_row(a.map, a.hkv, w.b, t);  // and the next three: pages are 16 n
+            if (row >= 0) {
+                row += (int64_t)h * a.map.page;
+                r.ok[i] = 1;
+                uint32_t cw[4], s[4], z[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    cw[x] = *reinterpret_cast<const uint32_t *>(a.vp.c + (row + x) * (D / 2) + dg * 4);
+                    const int64_t g = (row + x) * ng + dg * 8 / a.G;
+                    s[x] = a.vp.s[g];
+                    z[x] = a.vp.z[g];
+                    // tokens that no row sees take a weight of 0, and 0 times
+                    // what a slot holds that was never written may be NaN
+                    const bool seen = t + x < w.hi && (t + x >= w.low || t + x < a.sinks);
+                    s[x] = seen ? s[x] : 0;
+                    z[x] = seen ? z[x] : 0;
+                }
+                r.c[i] = make_uint4(cw[0], cw[1], cw[2], cw[3]);
+                r.sc[i][0] = s[0] | (s[1] << 16);
+                r.sc[i][1] = s[2] | (s[3] << 16);
+                r.sc[i][2] = z[0] | (z[1] << 16);
+                r.sc[i][3] = z[2] | (z[3] << 16);
+            }
+        }
+    }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r)
+{
+    using A = Ahead<D, NT>;
+#pragma unroll
+    for (int i = 0; i < A::N; ++i) {
+        const int item = threadIdx.x + i * NT;
+        if (item < 2 * D) {
+            const int t = item / (D / 32), sl = item % (D / 32);
+            const h2v s = pair_of(r.sc[i][0], r.sc[i][0]), z = pair_of(r.sc[i][1], r.sc[i][1]);
+            const uint32_t w[4] = {r.c[i].x, r.c[i].y, r.c[i].z, r.c[i].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<uint4 *>(st.k + t * (2 * D) +
+                                           (((4 * sl + x) ^ (t & Stage<D>::KSW)) * 16)) =
+                    unpack8(w[x], s, z);
+            if (sl == 0 && (t & 15) == 0)
+                st.ok[t >> 4] = r.ok[i];
+        } else if (item < 4 * D) {
+            const int j = item - 2 * D;
+            const int q = j / (D / 8), dg = j % (D / 8);
+            // tokens 4 q .. 4 q + 3: 16-token group q / 4, lane half q % 2,
+            // 8-byte piece (q / 2) % 2
+            const int unit = (q >> 2) * 2 + (q & 1), piece = (q >> 1) & 1;
+            const h2v s01 = bits_h2(r.sc[i][0]), s23 = bits_h2(r.sc[i][1]);
+            const h2v z01 = bits_h2(r.sc[i][2]), z23 = bits_h2(r.sc[i][3]);
+#pragma unroll
+            for (int bt = 0; bt < 4; ++bt) {
+                // byte bt of two tokens in bytes 0 and 2
+                const uint32_t sel = (uint32_t)bt | 0x0C00u | ((uint32_t)(4 + bt) << 16) | 0x0C000000u;
+                const uint32_t x01 = perm_b32(r.c[i].y, r.c[i].x, sel);
+                const uint32_t x23 = perm_b32(r.c[i].w, r.c[i].z, sel);
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    const int d = dg * 8 + 2 * bt + hi;
+                    const h2v a01 = hi ? nib_pair<true>(x01) : nib_pair<false>(x01);
+                    const h2v a23 = hi ? nib_pair<true>(x23) : nib_pair<false>(x23);
+                    *reinterpret_cast<uint2 *>(st.v + d * (2 * TT) +
+                                               ((unit ^ ((d ^ (d >> 3)) & 7)) * 16) + piece * 8) =
+                        make_uint2(__builtin_bit_cast(uint32_t, fma2(a01, s01, z01)),
+                                   __builtin_bit_cast(uint32_t, fma2(a23, s23, z23)));
+                }
+            }
+        }
+    }
+}
+
+// Block id -> (slot, split, cache head): heads next to each other, so that
+// with eight of them each XCD keeps to one head's cache; late slots (long
+// rows of a prompt) first.
+struct Place {
+    int slot, split, h;
+};
+
+__device__ __forceinline__ Place place(const PagedAttnArgs &a, int slots)
+{
+    const uint32_t id = blockIdx.x;
+    const uint32_t rest = id / (uint32_t)a.hkv;
+    Place p;
+    p.h = (int)(id % (uint32_t)a.hkv);
+    p.split = (int)(rest % (uint32_t)a.splits);
+    p.slot = slots - 1 - (int)(rest / (uint32_t)a.splits);
+    return p;
+}
+
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slots)
+{
+    constexpr int NT = 64 * NW, MR = 32 * NW;
+    constexpr int KS = D / 16, DB = D / 32;
+    __shared__ __align__(16) Stage<D> st[2];
+    __shared__ int shb;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = lane & 31, hf = lane >> 5;
+    const Place pl = place(a, slots);
+    const Work w = find_work<MR>(a, pl.slot, &shb);
+    if (w.rows == 0 || pl.split >= w.used)
+        return;
+    const float inf = __builtin_inff();
+    const float c2 = a.sm_scale * 1.44269504088896340736f;  // log2(e)
+
+    // this lane's query: row, batch row, head, position
+    const int row = min(w.row0 + wave * 32 + n, w.rows - 1);
+    const bool live = w.row0 + wave * 32 + n < w.rows;
+    const int qi = row / a.rep;
+    const int head = pl.h * a.rep + (row - qi * a.rep);
+    const int p = w.pos0 + qi;
+    const int64_t trow = w.tok0 + qi;
+    const int wfirst = a.window > 0 ? p - a.window : -1;  // tokens up to here only as sinks
+    v8h qb[KS];
+    {
+        const uint16_t *qr = a.q + trow * a.q_stride + (int64_t)head * D;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            qb[k] = __builtin_bit_cast(
+                v8h, nib_order(*reinterpret_cast<const uint4 *>(qr + 16 * k + 8 * hf)));
+    }
+
+    v16f o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            o[d][r] = 0.0f;
+    float m = -inf, l = 0.0f;  // in log2 units; this lane's half of the sum
+
+    const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
+    auto token0 = [&](int i) { return paged::step_token(w, i); };
+    // the wave's smallest and largest position, for the steps that need no mask
+    const int pw0 = w.pos0 + min(w.row0 + wave * 32, w.rows - 1) / a.rep;
+    const int pw1 = w.pos0 + min(w.row0 + wave * 32 + 31, w.rows - 1) / a.rep;
+
+    Ahead<D, NT> ah;
+    if (begin < end) {
+        read_ahead<D, NT>(a, w, pl.h, token0(begin), ah);
+        put<D, NT>(st[0], ah);
+        __syncthreads();
+    }
+    for (int i = begin; i < end; ++i) {
+        const Stage<D> &cur = st[(i - begin) & 1];
+        const int t0 = token0(i);
+        if (i + 1 < end)
+            read_ahead<D, NT>(a, w, pl.h, token0(i + 1), ah);
+
+        // scores of 64 tokens: registers 8 x + r of s[u] hold token
+        // 32 u + 16 x + 8 (r / 4) + 4 hf + r % 4
+        v16f s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[u][r] = 0.0f;
+            const int t = 32 * u + n;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const v8h kf = *reinterpret_cast<const v8h *>(
+                    cur.k + t * (2 * D) + (((2 * k + hf) ^ (t & Stage<D>::KSW)) * 16));
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qb[k], s[u], 0, 0, 0);
+            }
+        }
+        const bool all = cur.ok[0] & cur.ok[1] & cur.ok[2] & cur.ok[3];
+        if (!all || t0 + TT - 1 > pw0 || (a.window > 0 && t0 <= pw1 - a.window)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int t = t0 + 32 * u + 8 * (r >> 2) + 4 * hf + (r & 3);
+                    const bool see = t <= p && (t > wfirst || t < a.sinks) && cur.ok[2 * u + (r >> 3)];
+                    s[u][r] = see ? s[u][r] : -inf;
+                }
+        }
+        float mt = s[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                mt = fmaxf(mt, s[u][r]);
+        {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt),
+                                                             false, false);
+            mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        }
+        const float mn = fmaxf(m, mt * c2);
+        const float ms = mn > -inf ? mn : 0.0f;  // nothing seen so far: weights 0
+        if (__any(mn > m)) {
+            const float f = __builtin_amdgcn_exp2f(m - ms);  // 0 on the first step
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    o[d][r] *= f;
+            m = mn;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                v8h pb;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * x + r], c2, -ms));
+                    l += e;
+                    pb[r] = (_Float16)e;
+                }
+                const int unit = (2 * u + x) * 2 + hf;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int dim = 32 * d + n;
+                    const v8h vf = *reinterpret_cast<const v8h *>(
+                        cur.v + dim * (2 * TT) + ((unit ^ ((dim ^ (dim >> 3)) & 7)) * 16));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pb, o[d], 0, 0, 0);
+                }
+            }
+        }
+        if (i + 1 < end)
+            put<D, NT>(st[(i + 1 - begin) & 1], ah);
+        __syncthreads();
+    }
+
+    {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false,
+                                                         false);
+        l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    }
+    if (!live)
+        return;
+    if (w.used == 1) {
+        const float f = l > 0.0f ? 1.0f / l : 0.0f;
+        uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                uint2 v;
+                v.x = (uint32_t)f2h(o[d][r] * f) | ((uint32_t)f2h(o[d][r + 1] * f) << 16);
+                v.y = (uint32_t)f2h(o[d][r + 2] * f) | ((uint32_t)f2h(o[d][r + 3] * f) << 16);
+                *reinterpret_cast<uint2 *>(dst + 32 * d + 2 * r + 4 * hf) = v;
+            }
+    } else {
+        const int64_t pr = (trow * a.hq + head) * a.splits + pl.split;
+        float *dst = a.part_o + pr * D;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<float4 *>(dst + 32 * d + 2 * r + 4 * hf) =
+                    make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+        if (hf == 0)
+            *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(m, l);
+    }
+}
+
+// The rows of a block whose splits were more than one: a wave per row.
+template <int D, int MR>
+__global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a, int slots)
+{
+    constexpr int E = D / 64;  // elements of a lane
+    __shared__ int shb;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int h = (int)(blockIdx.x % (uint32_t)a.hkv);
+    const Work w = find_work<MR>(a, (int)(blockIdx.x / (uint32_t)a.hkv), &shb);
+    if (w.rows == 0 || w.used == 1)
+        return;
+    for (int r = blockIdx.y * 4 + wave; r < MR && w.row0 + r < w.rows; r += gridDim.y * 4) {
+        const int row = w.row0 + r, qi = row / a.rep;
+        const int head = h * a.rep + (row - qi * a.rep);
+        const int64_t trow = w.tok0 + qi;
+        const int64_t pr = (trow * a.hq + head) * a.splits;
+        float mx = -__builtin_inff();
+        for (int s = lane; s < w.used; s += 64)
+            mx = fmaxf(mx, a.part_ml[2 * (pr + s)]);
+        static_for<6>([&](auto J) { mx = lane_max<J>(mx); });
+        const float ms = mx > -__builtin_inff() ? mx : 0.0f;
+        float l = 0.0f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            o[e] = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < w.used; ++s) {
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (pr + s));
+            const float f = __builtin_amdgcn_exp2f(ml.x - ms);  // 0 where it saw nothing
+            l = __builtin_fmaf(ml.y, f, l);
+            const float *src = a.part_o + (pr + s) * D + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                o[e] = __builtin_fmaf(src[e], f, o[e]);
+        }
+        const float f = l > 0.0f ? 1.0f / l : 0.0f;
+        uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            dst[e] = f2h(o[e] * f);
+    }
+}
+
+template <int D, int NW>
+hipError_t go_tile(const PagedAttnArgs &a, hipStream_t s)
+{
+    constexpr int MR = 32 * NW;
+    const int slots = (int)paged::slots(a.map.T, a.map.B, a.rep, MR);
+    const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
+    hipLaunchKernelGGL((k_paged_tile<D, NW>), grid, dim3(64 * NW), 0, s, a, slots);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1)
+        return e;
+    const dim3 cgrid((unsigned)(slots * a.hkv), (unsigned)std::max(1, MR / 32));
+    hipLaunchKernelGGL((k_paged_combine<D, MR>), cgrid, dim3(256), 0, s, a, slots);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t go_rows(const PagedAttnArgs &a, int rows, hipStream_t s)
+{
+    if constexpr (D < 256) {
+        if (rows == 64)
+            return go_tile<D, 2>(a, s);
+        if (rows == 256)
+            return go_tile<D, 8>(a, s);
+    }
+    return rows == 128 ? go_tile<D, 4>(a, s) : hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedAttnArgs &a, const paged::Plan &p, hipStream_t s)
+{
+    switch (a.D) {
+    case 64: return go_rows<64>(a, p.rows, s);
+    case 128: return go_rows<128>(a, p.rows, s);
+    case 256: return go_rows<256>(a, p.rows, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace quarot

@@ -1,0 +1,130 @@
+// The arithmetic of the paged attention's work: positions to pages, the blocks
+// of a ragged batch, the steps of a block and their split, and the host's choice
+// of kernel.  Plain C++ with no HIP, so that it builds and is checked on any
+// host; what kernels run of it is marked QUAROT_HD.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+#if defined(__HIP__)
+#define QUAROT_HD __host__ __device__ inline
+#else
+#define QUAROT_HD inline
+#endif
+
+namespace quarot {
+namespace paged {
+
+constexpr int STEP = 64;          // tokens of a step
+constexpr int MIN_STEPS = 4;      // of a split
+constexpr int MAX_THREADS = 512;  // of an attention block
+
+// t / page = (t * mul >> 32) >> sh for 0 <= t < 2^31: with L = ceil(log2(page))
+// and mul = floor(2^(31 + L) / page) + 1 (below 2^32, page >= 2),
+// t mul / 2^(31 + L) exceeds t / page by less than 1 / page, which changes no
+// quotient.
+struct Divisor {
+    uint32_t mul;
+    int sh;
+};
+
+inline Divisor divisor(int page)
+{
+    int L = 1;
+    while ((int64_t(1) << L) < page)
+        ++L;
+    return Divisor{(uint32_t)(((uint64_t)1 << (31 + L)) / (uint64_t)page + 1), L - 1};
+}
+
+// Blocks of MR query rows (new tokens times query heads of a cache head) of a
+// ragged batch: sequence b takes the slots from first_slot(cu[b] rep, b, MR) to
+// that of b + 1, at least as many as its rows fill (the floor of a sum is no
+// less than the sum of floors, and b adds one for each sequence), so a block
+// finds its sequence from two entries of cu and no sum over those before it.
+QUAROT_HD int64_t first_slot(int64_t rows_before, int64_t b, int mr)
+{
+    return rows_before / mr + b;
+}
+
+// What a block works on.
+struct Span {
+    int row0, rows;  // first row, rows of the sequence; rows 0: nothing to do
+    int pos0;        // position of the sequence's first new token
+    int hi, low;     // tokens low .. hi - 1 and the sinks are seen by some row
+    int lo, first;   // steps 0 .. lo - 1 are sinks, step i >= lo is token block i - lo + first
+    int steps;       // in all
+    int per, used;   // steps of a split, splits that have any (1 at least)
+};
+
+// Sequence of rows cu0 .. cu1 - 1 of a batch of T, len cached tokens; block
+// `slot - first_slot` of it; a table of cap positions; window 0: none; at most
+// `splits` splits.  Any content of cu0, cu1 and len gives a span inside the
+// batch and the table.  cap and T are at most 2^30, window and sinks too.
+QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t block, int mr,
+                    int window, int sinks, int splits)
+{
+    Span w = {};
+    const int64_t row0 = block * mr, rows = ((int64_t)cu1 - cu0) * rep;
+    w.used = 1;
+    if (cu0 < 0 || cu1 > T || block < 0 || row0 >= rows)
+        return w;
+    const int n = cu1 - cu0;
+    len = len < 0 ? 0 : len;
+    w.row0 = (int)row0;
+    w.rows = (int)rows;
+    w.pos0 = len - n;
+    const int last = (int)(row0 + mr < rows ? row0 + mr : rows) - 1;
+    const int p0 = w.pos0 + w.row0 / rep, p1 = w.pos0 + last / rep;
+    w.hi = p1 + 1 > cap ? cap : p1 + 1 < 0 ? 0 : p1 + 1;
+    w.steps = (w.hi + STEP - 1) / STEP;
+    if (window > 0) {
+        w.low = p0 - window + 1 < 0 ? 0 : p0 - window + 1 > w.hi ? w.hi : p0 - window + 1;
+        w.first = w.low / STEP;
+        w.lo = ((sinks < w.hi ? sinks : w.hi) + STEP - 1) / STEP;
+        w.lo = w.lo < w.first ? w.lo : w.first;
+        w.steps += w.lo - w.first;
+    }
+    w.per = (w.steps + splits - 1) / splits;
+    w.per = w.per > MIN_STEPS ? w.per : MIN_STEPS;
+    w.used = (w.steps + w.per - 1) / w.per;
+    w.used = w.used > 1 ? w.used : 1;
+    return w;
+}
+
+// First token of step i.
+QUAROT_HD int step_token(const Span &w, int i)
+{
+    return (i < w.lo ? i : i - w.lo + w.first) * STEP;
+}
+
+struct Plan {
+    int rows;    // query rows of a block
+    int splits;  // blocks that share a block row's tokens, at most
+};
+
+// T new tokens of B sequences, hkv cache heads with rep query heads each, at
+// most max_len cached tokens.  Only a rule of speed: any content of cu and len
+// is right under any plan.
+inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int64_t max_len,
+                 int64_t window, int64_t sinks)
+{
+    Plan p;
+    // query rows of a sequence, on average
+    const int64_t rows = (T * rep + B - 1) / B;
+    p.rows = D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    const int64_t blocks = B * ((rows + p.rows - 1) / p.rows) * hkv;
+    const int64_t seen = window > 0 ? std::min(max_len, window + sinks + T / B) : max_len;
+    const int64_t most = std::max<int64_t>(1, (seen + 255) / 256);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 512 / blocks, 128}));
+    return p;
+}
+
+// Blocks of a launch along the sequences.
+inline int64_t slots(int64_t T, int64_t B, int64_t rep, int mr)
+{
+    return T * rep / mr + B;
+}
+
+}  // namespace paged
+}  // namespace quarot
