@@ -616,8 +616,8 @@ quarot_status quarot_kv_append_paged(const quarot_f16 *q, int64_t q_stride, quar
  */
 size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_t n_heads,
                                                 int64_t n_kv_heads, int64_t head_dim,
-                                                int64_t max_seq_len, int64_t window,
-                                                int64_t n_sinks);
+                                                int64_t group, int64_t max_seq_len,
+                                                int64_t window, int64_t n_sinks);
 
 /*
  * Attention of the new tokens over the pages (§4 Stage 2c with App. A.10's

@@ -102,7 +102,7 @@ SIGNATURES = {
     "quarot_rope": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I, _P]),
     "quarot_kv_append_paged": (_I, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _I64, _I64,
                                     _I, _I, _F, _P]),
-    "quarot_kv_paged_attention_workspace_size": (ctypes.c_size_t, [_I64] * 8),
+    "quarot_kv_paged_attention_workspace_size": (ctypes.c_size_t, [_I64] * 9),
     "quarot_kv_paged_attention": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _F,
                                        _P, ctypes.c_size_t, _P]),
 }
@@ -1074,9 +1074,12 @@ def quarot_kv_append_paged(k: torch.Tensor, v: torch.Tensor, k_cache, v_cache,
 
 def quarot_kv_paged_attention_workspace_size(T: int, batch: int, n_heads: int, n_kv_heads: int,
                                              head_dim: int, max_seq_len: int, window: int = 0,
-                                             n_sinks: int = 0) -> int:
+                                             n_sinks: int = 0,
+                                             group: Optional[int] = None) -> int:
+    """Bytes of workspace (group None: one group per row, head_dim)."""
     return int(lib().quarot_kv_paged_attention_workspace_size(
-        T, batch, n_heads, n_kv_heads, head_dim, max_seq_len, window, n_sinks))
+        T, batch, n_heads, n_kv_heads, head_dim, head_dim if group is None else group, max_seq_len,
+        window, n_sinks))
 
 
 def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: torch.Tensor,
@@ -1106,7 +1109,7 @@ def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: tor
     (qp, qs), (op, ost) = _token_rows(q, "q"), _token_rows(out, "out")
     if workspace is None:
         need = quarot_kv_paged_attention_workspace_size(
-            T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks)
+            T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks, group)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check("quarot_kv_paged_attention", lib().quarot_kv_paged_attention(

@@ -205,14 +205,14 @@ quarot_status quarot_kv_append_paged(const quarot_f16 *q, int64_t q_stride, quar
 
 size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_t n_heads,
                                                 int64_t n_kv_heads, int64_t head_dim,
-                                                int64_t max_seq_len, int64_t window,
+                                                int64_t group, int64_t max_seq_len, int64_t window,
                                                 int64_t n_sinks)
 {
     if (T <= 0 || T > kMaxTokens || batch <= 0 || batch > 0xFFFFFF || n_heads <= 0 ||
         n_heads > 0xFFFF || n_kv_heads <= 0 || n_heads % n_kv_heads || !head_dim_ok(head_dim) ||
-        max_seq_len <= 0 || window < 0 || n_sinks < 0)
+        group <= 0 || max_seq_len <= 0 || window < 0 || n_sinks < 0)
         return 0;
-    const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim,
+    const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim, group,
                                    std::min(max_seq_len, kMaxTokens), std::min(window, kMaxTokens),
                                    std::min(n_sinks, kMaxTokens));
     return attention_workspace(p, T, n_heads, head_dim);
@@ -246,7 +246,7 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
     window = std::min(window, kMaxTokens);
     n_sinks = std::min(n_sinks, kMaxTokens);
     const paged::Plan p = paged::plan(T, cache->batch, cache->n_kv_heads, n_heads / cache->n_kv_heads,
-                                   D, std::min(max_seq_len, kMaxTokens), window, n_sinks);
+                                   D, cache->group, std::min(max_seq_len, kMaxTokens), window, n_sinks);
     // a launch holds fewer than 2^32 threads
     const int64_t slots = paged::slots(T, cache->batch, n_heads / cache->n_kv_heads, p.rows);
     if (slots * cache->n_kv_heads * p.splits > 0xFFFFFFFFll / paged::MAX_THREADS)
@@ -273,6 +273,7 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
     a.sinks = (int)n_sinks;
     a.sm_scale = sm_scale;
     a.splits = p.splits;
+    a.least = p.least;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = a.part_o + (size_t)T * n_heads * p.splits * D;
     hipError_t e = launch_paged_attention(a, p, (hipStream_t)stream);

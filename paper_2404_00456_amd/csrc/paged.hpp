@@ -68,7 +68,7 @@ struct PagedAttnArgs {
     int D, G;
     int window, sinks;  // window 0: none
     float sm_scale;
-    int splits;
+    int splits, least;  // of paged::Plan
     float *part_o;      // [T * hq, splits, D]
     float *part_ml;     // [T * hq, splits, 2]: maximum (in log2 units), sum
 };

@@ -56,7 +56,7 @@ __device__ __forceinline__ Work find_work(const PagedAttnArgs &a, int slot, int 
     static_cast<paged::Span &>(w) =
         paged::span(c0, c1, m.len[w.b], m.T, m.max_pages * m.page, a.rep,
                     slot - paged::first_slot((int64_t)c0 * a.rep, w.b, MR), MR, a.window, a.sinks,
-                    a.splits);
+                    a.splits, a.least);
     w.tok0 = c0;
     return w;
 }
@@ -417,33 +417,333 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
     }
 }
 
-// The rows of a block whose splits were more than one: a wave per row.
-template <int D, int MR>
-__global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a, int slots)
+// ---- few query rows: single tokens, and a few that were guessed ahead -------
+//
+// k_paged_rows: up to 16 query rows (new tokens times the heads of a cache head)
+// of a sequence, one group per cached row.  Four waves take the block's token
+// blocks of 64 in turn, straight from memory to registers, 16 tokens at a time
+// as in the dense decode kernels: A = the K codes as fp16 integers against B =
+// the queries, then A = the weights against B = the V codes.  Codes enter as
+// they are, so that nothing of a key or value is rounded:
+//   q . khat_t = ks_t (q . code_t) + kz_t sum(q),
+//   sum_t p_t vhat_t = sum_t (p_t vs_t) code_t + sum_t p_t vz_t.
+// The weights p_t vs_t are two bf16 parts (16 bits; bf16 holds them whatever the
+// values' scale is, where fp16 would lose small ones), each an A operand of its
+// own.  A code c is or-ed into a significand: 64 + c in the K operand (fp16
+// 0x5400, values spaced by 1/16), 128 + c in the V operand (bf16 0x4300, spaced
+// by 1); what the offset adds is taken off in binary32, 64 sum(q) from a score and 128 times the
+// sum of the weights as they were multiplied (a product with ones) from an
+// output: an offset of 64 or 128 costs 6 or 7 of binary32's 24 bits.
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+constexpr int ROWS_W = 4;  // waves
+
+template <int D>
+__global__ __launch_bounds__(64 * ROWS_W) void k_paged_rows(PagedAttnArgs a, int slots)
+{
+    constexpr int MR = paged::FEW_ROWS;
+    constexpr int KW = D / 32;  // dwords of K codes of a lane: D / 4 elements of a token
+    constexpr int VD = D / 16;  // dimensions of a lane in the value product
+    constexpr float RAISE = 16.0f;  // a maximum moves when a score passes it by 2^16
+    __shared__ float red[ROWS_W][MR][D + 2];
+    __shared__ int shb;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = lane & 15, g = lane >> 4;
+    const Place pl = place(a, slots);
+    const Work w = find_work<MR>(a, pl.slot, &shb);
+    if (w.rows == 0 || pl.split >= w.used)
+        return;
+    const float inf = __builtin_inff();
+    const float c2 = a.sm_scale * 1.44269504088896340736f;  // log2(e)
+    const int R = min(MR, w.rows - w.row0);
+
+    // this lane's query (column n of the scores)
+    const int row = w.row0 + min(n, R - 1), qi = row / a.rep;
+    const int p = w.pos0 + qi;
+    const int wfirst = a.window > 0 ? p - a.window : -1;
+    const int pmin = w.pos0 + w.row0 / a.rep, pmax = w.pos0 + (w.row0 + R - 1) / a.rep;
+    v8h qb[KW];
+    float qsum = 0.0f;
+    {
+        const uint16_t *qr = a.q + (int64_t)(w.tok0 + qi) * a.q_stride +
+                             (int64_t)(pl.h * a.rep + (row - qi * a.rep)) * D + (D / 4) * g;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            qb[k] = __builtin_bit_cast(v8h, nib_order(*reinterpret_cast<const uint4 *>(qr + 8 * k)));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                qsum += (float)qb[k][e];
+        }
+        float2 t = lane_pair_swap<4>(qsum);
+        qsum = t.x + t.y;
+        t = lane_pair_swap<5>(qsum);
+        qsum = t.x + t.y;
+    }
+    const float qs = qsum * c2, q64 = -64.0f * qsum;
+
+    v4f o[VD], o1 = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int d = 0; d < VD; ++d)
+        o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -inf, l = 0.0f, zs = 0.0f;
+
+    const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
+    for (int i0 = begin + wave; i0 < end; i0 += ROWS_W * 16) {
+        // the pool rows of the next 16 steps' 64 groups of 16 tokens, one a lane
+        int64_t base = -1;
+        {
+            const int i = i0 + (lane >> 2) * ROWS_W;
+            if (i < end) {
+                const int t = paged::step_token(w, i) + 16 * (lane & 3);
+                if (t < w.hi)
+                    base = pool_row(a.map, a.hkv, w.b, t);
+                if (base >= 0)
+                    base += (int64_t)pl.h * a.map.page;
+            }
+        }
+#pragma unroll 1
+        for (int j = 0; j < 16 && i0 + j * ROWS_W < end; ++j) {
+            const int t0 = paged::step_token(w, i0 + j * ROWS_W);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int th = t0 + 32 * half;
+                uint32_t kc[2][KW], vc[2][4][(VD + 7) / 8];
+                uint2 ks[2], kz[2], vs[2], vz[2];
+                bool ok[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int src = 4 * j + 2 * half + u;
+                    const uint32_t blo = __builtin_amdgcn_readlane((uint32_t)base, src);
+                    const uint32_t bhi = __builtin_amdgcn_readlane((uint32_t)(base >> 32), src);
+                    const int64_t b0 = (int64_t)(((uint64_t)bhi << 32) | blo);
+                    ok[u] = b0 >= 0;
+                    const int64_t r0 = ok[u] ? b0 : 0;  // a row of the pool, masked below
+                    const uint8_t *kp = a.kp.c + r0 * (D / 2) + (n * (D / 2) + g * (D / 8));
+                    const uint8_t *vp = a.vp.c + r0 * (D / 2) + (4 * g * (D / 2) + n * (D / 32));
+                    __builtin_memcpy(kc[u], __builtin_assume_aligned(kp, D / 8 < 16 ? D / 8 : 16),
+                                     4 * KW);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if constexpr (D == 64)
+                            vc[u][t][0] = *reinterpret_cast<const uint16_t *>(vp + t * (D / 2));
+                        else
+                            __builtin_memcpy(vc[u][t], __builtin_assume_aligned(vp + t * (D / 2), D / 32),
+                                             D / 32);
+                    ks[u] = *reinterpret_cast<const uint2 *>(a.kp.s + r0 + 4 * g);
+                    kz[u] = *reinterpret_cast<const uint2 *>(a.kp.z + r0 + 4 * g);
+                    vs[u] = *reinterpret_cast<const uint2 *>(a.vp.s + r0 + 4 * g);
+                    vz[u] = *reinterpret_cast<const uint2 *>(a.vp.z + r0 + 4 * g);
+                }
+                float x[2][4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    v4f acc = {q64, q64, q64, q64};
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) {
+                        const uint32_t wd = kc[u][k];
+                        auto f64 = [](uint32_t b) { return (b & 0x00F000F0u) | 0x54005400u; };
+                        const uint4 kf = make_uint4(f64(wd << 4), f64(wd), f64(wd >> 4), f64(wd >> 8));
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, kf), qb[k],
+                                                                     acc, 0, 0, 0);
+                    }
+                    const h2v s01 = bits_h2(ks[u].x), s23 = bits_h2(ks[u].y);
+                    const h2v z01 = bits_h2(kz[u].x), z23 = bits_h2(kz[u].y);
+                    const float sf[4] = {(float)s01[0], (float)s01[1], (float)s23[0], (float)s23[1]};
+                    const float zf[4] = {(float)z01[0], (float)z01[1], (float)z23[0], (float)z23[1]};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        x[u][r] = __builtin_fmaf(sf[r], acc[r] * c2, zf[r] * qs);
+                }
+                if (!(ok[0] & ok[1]) || th + 31 > pmin || (a.window > 0 && th <= pmax - a.window)) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t keep[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int t = th + 16 * u + 4 * g + r;
+                            const bool see = ok[u] && t <= p && (t > wfirst || t < a.sinks);
+                            x[u][r] = see ? x[u][r] : -inf;
+                            keep[r] = see ? 0xFFFFu : 0u;
+                        }
+                        // a weight of 0 times what a slot that was never written
+                        // holds may be NaN
+                        const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
+                        vs[u].x &= k01;
+                        vs[u].y &= k23;
+                        vz[u].x &= k01;
+                        vz[u].y &= k23;
+                    }
+                }
+                float mt = x[0][0];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        mt = fmaxf(mt, x[u][r]);
+                if (__any(mt > m + RAISE)) {  // always where m is -inf and a token is seen
+                    mt = lane_max<4>(mt);
+                    mt = lane_max<5>(mt);
+                    const float mn = fmaxf(m, mt);
+                    const float f = __builtin_amdgcn_exp2f(m - (mn > -inf ? mn : 0.0f));
+                    m = mn;
+                    l *= f;
+                    zs *= f;
+                    float fr[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        fr[r] = __shfl(f, 4 * g + r);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        o1[r] *= fr[r];
+#pragma unroll
+                        for (int d = 0; d < VD; ++d)
+                            o[d][r] *= fr[r];
+                    }
+                }
+                const float ms = m > -inf ? m : 0.0f;
+                uint32_t hh[4], ll[4];  // weights of the 32 tokens, as bf16 pairs
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const h2v s01 = bits_h2(vs[u].x), s23 = bits_h2(vs[u].y);
+                    const h2v z01 = bits_h2(vz[u].x), z23 = bits_h2(vz[u].y);
+                    const float sf[4] = {(float)s01[0], (float)s01[1], (float)s23[0], (float)s23[1]};
+                    const float zf[4] = {(float)z01[0], (float)z01[1], (float)z23[0], (float)z23[1]};
+                    uint32_t wb[4], rb[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = __builtin_amdgcn_exp2f(x[u][r] - ms);
+                        l += e;
+                        zs = __builtin_fmaf(e, zf[r], zs);
+                        const float wt = e * sf[r];
+                        wb[r] = __float_as_uint(wt);
+                        rb[r] = __float_as_uint(wt - __uint_as_float(wb[r] & 0xFFFF0000u));
+                    }
+                    hh[2 * u] = perm_b32(wb[1], wb[0], 0x07060302u);
+                    hh[2 * u + 1] = perm_b32(wb[3], wb[2], 0x07060302u);
+                    ll[2 * u] = perm_b32(rb[1], rb[0], 0x07060302u);
+                    ll[2 * u + 1] = perm_b32(rb[3], rb[2], 0x07060302u);
+                }
+                const v8bf wh = __builtin_bit_cast(v8bf, make_uint4(hh[0], hh[1], hh[2], hh[3]));
+                const v8bf wl = __builtin_bit_cast(v8bf, make_uint4(ll[0], ll[1], ll[2], ll[3]));
+                const v8bf ones = __builtin_bit_cast(
+                    v8bf, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+                o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, ones, o1, 0, 0, 0);
+                o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, ones, o1, 0, 0, 0);
+#pragma unroll
+                for (int bt = 0; bt < VD / 2; ++bt) {
+                    // byte bt of tokens 4 g, 4 g + 1 (and + 2, + 3) of both groups
+                    const int wd = bt / 4;
+                    const uint32_t sel = (uint32_t)(bt & 3) | 0x0C00u |
+                                         ((uint32_t)(4 + (bt & 3)) << 16) | 0x0C000000u;
+                    uint32_t lo[4], hi[4];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t b2 = perm_b32(vc[u][2 * e + 1][wd], vc[u][2 * e][wd], sel);
+                            lo[2 * u + e] = (b2 & 0x000F000Fu) | 0x43004300u;
+                            hi[2 * u + e] = ((b2 >> 4) & 0x000F000Fu) | 0x43004300u;
+                        }
+                    const v8bf vlo = __builtin_bit_cast(v8bf, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                    const v8bf vhi = __builtin_bit_cast(v8bf, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                    o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, vlo, o[2 * bt], 0, 0, 0);
+                    o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, vlo, o[2 * bt], 0, 0, 0);
+                    o[2 * bt + 1] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, vhi, o[2 * bt + 1], 0, 0, 0);
+                    o[2 * bt + 1] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // each wave's (maximum, sum, output) of its rows in LDS, then one of all
+    {
+        float2 t = lane_pair_swap<4>(l);
+        l = t.x + t.y;
+        t = lane_pair_swap<5>(l);
+        l = t.x + t.y;
+        t = lane_pair_swap<4>(zs);
+        zs = t.x + t.y;
+        t = lane_pair_swap<5>(zs);
+        zs = t.x + t.y;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float z = __shfl(zs, 4 * g + r);
+#pragma unroll
+        for (int d = 0; d < VD; ++d)
+            red[wave][4 * g + r][VD * n + d] = __builtin_fmaf(-128.0f, o1[r], o[d][r]) + z;
+    }
+    if (g == 0) {
+        red[wave][n][D] = m;
+        red[wave][n][D + 1] = l;
+    }
+    __syncthreads();
+    for (int i = tid; i < R * (D / 2); i += 64 * ROWS_W) {
+        const int r = i / (D / 2), d = 2 * (i % (D / 2));
+        float mx = -inf;
+#pragma unroll
+        for (int v = 0; v < ROWS_W; ++v)
+            mx = fmaxf(mx, red[v][r][D]);
+        const float ms = mx > -inf ? mx : 0.0f;
+        float lt = 0.0f, oa = 0.0f, ob = 0.0f;
+#pragma unroll
+        for (int v = 0; v < ROWS_W; ++v) {
+            const float f = __builtin_amdgcn_exp2f(red[v][r][D] - ms);
+            lt = __builtin_fmaf(red[v][r][D + 1], f, lt);
+            oa = __builtin_fmaf(red[v][r][d], f, oa);
+            ob = __builtin_fmaf(red[v][r][d + 1], f, ob);
+        }
+        const int rr = w.row0 + r, ti = rr / a.rep;
+        const int64_t trow = w.tok0 + ti;
+        const int head = pl.h * a.rep + (rr - ti * a.rep);
+        if (w.used == 1) {
+            const float f = lt > 0.0f ? 1.0f / lt : 0.0f;
+            *reinterpret_cast<uint32_t *>(a.out + trow * a.out_stride + (int64_t)head * D + d) =
+                (uint32_t)f2h(oa * f) | ((uint32_t)f2h(ob * f) << 16);
+        } else {
+            const int64_t pr = (trow * a.hq + head) * a.splits + pl.split;
+            *reinterpret_cast<float2 *>(a.part_o + pr * D + d) = make_float2(oa, ob);
+            if (d == 0)
+                *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(mx, lt);
+        }
+    }
+}
+
+// The rows of a block whose splits were more than one.  WPR waves share a row's
+// splits: one where there are few of them, four where one after the other they
+// would cost a memory latency each.
+template <int D, int MR, int WPR>
+__global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a)
 {
     constexpr int E = D / 64;  // elements of a lane
+    constexpr int RPB = 4 / WPR;
     __shared__ int shb;
+    __shared__ float red[WPR > 1 ? 4 : 1][D + 2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = (int)(blockIdx.x % (uint32_t)a.hkv);
     const Work w = find_work<MR>(a, (int)(blockIdx.x / (uint32_t)a.hkv), &shb);
     if (w.rows == 0 || w.used == 1)
         return;
-    for (int r = blockIdx.y * 4 + wave; r < MR && w.row0 + r < w.rows; r += gridDim.y * 4) {
-        const int row = w.row0 + r, qi = row / a.rep;
+    const float inf = __builtin_inff();
+    for (int r0 = blockIdx.y * RPB; r0 < MR && w.row0 + r0 < w.rows; r0 += gridDim.y * RPB) {
+        const int r = r0 + wave / WPR, row = min(w.row0 + r, w.rows - 1), qi = row / a.rep;
+        const bool live = r < MR && w.row0 + r < w.rows;
         const int head = h * a.rep + (row - qi * a.rep);
         const int64_t trow = w.tok0 + qi;
         const int64_t pr = (trow * a.hq + head) * a.splits;
-        float mx = -__builtin_inff();
+        float mx = -inf;
         for (int s = lane; s < w.used; s += 64)
             mx = fmaxf(mx, a.part_ml[2 * (pr + s)]);
         static_for<6>([&](auto J) { mx = lane_max<J>(mx); });
-        const float ms = mx > -__builtin_inff() ? mx : 0.0f;
+        const float ms = mx > -inf ? mx : 0.0f;
         float l = 0.0f, o[E];
 #pragma unroll
         for (int e = 0; e < E; ++e)
             o[e] = 0.0f;
-#pragma unroll 4
-        for (int s = 0; s < w.used; ++s) {
+#pragma unroll 8
+        for (int s = wave % WPR; s < w.used; s += WPR) {
             const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (pr + s));
             const float f = __builtin_amdgcn_exp2f(ml.x - ms);  // 0 where it saw nothing
             l = __builtin_fmaf(ml.y, f, l);
@@ -452,12 +752,42 @@ __global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a, int slot
             for (int e = 0; e < E; ++e)
                 o[e] = __builtin_fmaf(src[e], f, o[e]);
         }
-        const float f = l > 0.0f ? 1.0f / l : 0.0f;
-        uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D + lane * E;
+        if constexpr (WPR > 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            dst[e] = f2h(o[e] * f);
+            for (int e = 0; e < E; ++e)
+                red[wave][lane * E + e] = o[e];
+            if (lane == 0)
+                red[wave][D] = l;
+            __syncthreads();
+            l = red[0][D] + red[1][D] + red[2][D] + red[3][D];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int i = lane * E + e;
+                o[e] = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+            }
+            __syncthreads();
+        }
+        if (live && wave % WPR == 0) {
+            const float f = l > 0.0f ? 1.0f / l : 0.0f;
+            uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D + lane * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                dst[e] = f2h(o[e] * f);
+        }
     }
+}
+
+template <int D, int MR>
+hipError_t go_combine(const PagedAttnArgs &a, int slots, hipStream_t s)
+{
+    const unsigned x = (unsigned)(slots * a.hkv);
+    if (a.splits > 8)
+        hipLaunchKernelGGL((k_paged_combine<D, MR, 4>), dim3(x, (unsigned)std::min(MR, a.rep * 4)),
+                           dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_paged_combine<D, MR, 1>), dim3(x, (unsigned)std::max(1, MR / 32)),
+                           dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 template <int D, int NW>
@@ -470,14 +800,25 @@ hipError_t go_tile(const PagedAttnArgs &a, hipStream_t s)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1)
         return e;
-    const dim3 cgrid((unsigned)(slots * a.hkv), (unsigned)std::max(1, MR / 32));
-    hipLaunchKernelGGL((k_paged_combine<D, MR>), cgrid, dim3(256), 0, s, a, slots);
-    return hipGetLastError();
+    return go_combine<D, MR>(a, slots, s);
+}
+
+template <int D>
+hipError_t go_few(const PagedAttnArgs &a, hipStream_t s)
+{
+    constexpr int MR = paged::FEW_ROWS;
+    const int slots = (int)paged::slots(a.map.T, a.map.B, a.rep, MR);
+    const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
+    hipLaunchKernelGGL((k_paged_rows<D>), grid, dim3(64 * ROWS_W), 0, s, a, slots);
+    hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.splits == 1 ? e : go_combine<D, MR>(a, slots, s);
 }
 
 template <int D>
 hipError_t go_rows(const PagedAttnArgs &a, int rows, hipStream_t s)
 {
+    if (rows == paged::FEW_ROWS)
+        return go_few<D>(a, s);
     if constexpr (D < 256) {
         if (rows == 64)
             return go_tile<D, 2>(a, s);

@@ -17,7 +17,7 @@ namespace quarot {
 namespace paged {
 
 constexpr int STEP = 64;          // tokens of a step
-constexpr int MIN_STEPS = 4;      // of a split
+constexpr int FEW_ROWS = 16;      // query rows of a block of the kernel for single tokens
 constexpr int MAX_THREADS = 512;  // of an attention block
 
 // t / page = (t * mul >> 32) >> sh for 0 <= t < 2^31: with L = ceil(log2(page))
@@ -59,10 +59,10 @@ struct Span {
 
 // Sequence of rows cu0 .. cu1 - 1 of a batch of T, len cached tokens; block
 // `slot - first_slot` of it; a table of cap positions; window 0: none; at most
-// `splits` splits.  Any content of cu0, cu1 and len gives a span inside the
+// `splits` splits of `least` steps each, or more where they would not do.  Any content of cu0, cu1 and len gives a span inside the
 // batch and the table.  cap and T are at most 2^30, window and sinks too.
 QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t block, int mr,
-                    int window, int sinks, int splits)
+                    int window, int sinks, int splits, int least)
 {
     Span w = {};
     const int64_t row0 = block * mr, rows = ((int64_t)cu1 - cu0) * rep;
@@ -86,7 +86,7 @@ QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t 
         w.steps += w.lo - w.first;
     }
     w.per = (w.steps + splits - 1) / splits;
-    w.per = w.per > MIN_STEPS ? w.per : MIN_STEPS;
+    w.per = w.per > least ? w.per : least;
     w.used = (w.steps + w.per - 1) / w.per;
     w.used = w.used > 1 ? w.used : 1;
     return w;
@@ -101,22 +101,31 @@ QUAROT_HD int step_token(const Span &w, int i)
 struct Plan {
     int rows;    // query rows of a block
     int splits;  // blocks that share a block row's tokens, at most
+    int least;   // steps of a split, at least
 };
 
 // T new tokens of B sequences, hkv cache heads with rep query heads each, at
 // most max_len cached tokens.  Only a rule of speed: any content of cu and len
 // is right under any plan.
-inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int64_t max_len,
-                 int64_t window, int64_t sinks)
+inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int64_t G,
+                 int64_t max_len, int64_t window, int64_t sinks)
 {
     Plan p;
     // query rows of a sequence, on average
     const int64_t rows = (T * rep + B - 1) / B;
+    const int64_t seen = window > 0 ? std::min(max_len, window + sinks + T / B) : max_len;
+    const int64_t steps = (seen + STEP - 1) / STEP;
+    if (rows <= FEW_ROWS && G == D) {
+        p.rows = FEW_ROWS;
+        const int64_t want = std::max<int64_t>(1, 2048 / (B * hkv));
+        p.least = (int)std::min<int64_t>(32, std::max<int64_t>(4, (steps + want - 1) / want));
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((steps + p.least - 1) / p.least, 128));
+        return p;
+    }
     p.rows = D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
     const int64_t blocks = B * ((rows + p.rows - 1) / p.rows) * hkv;
-    const int64_t seen = window > 0 ? std::min(max_len, window + sinks + T / B) : max_len;
-    const int64_t most = std::max<int64_t>(1, (seen + 255) / 256);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 512 / blocks, 128}));
+    p.least = 4;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, 512 / blocks, 128}));
     return p;
 }
 

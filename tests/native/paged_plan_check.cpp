@@ -56,7 +56,7 @@ static void batches(std::mt19937 &rng)
         const int B = 1 + rng() % 6, rep = 1 + rng() % 9;
         const int mr = std::vector<int>{16, 64, 128, 256}[rng() % 4];
         const int window = rng() % 3 ? 0 : 1 + rng() % 300, sinks = rng() % 90;
-        const int splits = 1 + rng() % 9;
+        const int splits = 1 + rng() % 9, least = 1 + rng() % 6;
         std::vector<int> cu(B + 1, 0), len(B);
         for (int b = 0; b < B; ++b) {
             const int n = rng() % 4 ? rng() % 5 : rng() % 400;
@@ -72,11 +72,12 @@ static void batches(std::mt19937 &rng)
                 if (f > slot || slot >= first_slot((int64_t)cu[b + 1] * rep, b + 1, mr))
                     continue;
                 const Span w = span(cu[b], cu[b + 1], len[b], T, cap, rep, slot - f, mr, window, sinks,
-                                    splits);
+                                    splits, least);
                 CHECK(w.used >= 1 && w.used <= splits, "used %d of %d", w.used, splits);
                 if (!w.rows)
                     continue;
-                CHECK(w.per * w.used >= w.steps && w.per * (w.used - 1) <= w.steps, "steps");
+                CHECK(w.per >= least && w.per * w.used >= w.steps && w.per * (w.used - 1) <= w.steps,
+                      "steps");
                 std::vector<char> walked((size_t)(std::max(w.hi, 0) + 2 * STEP), 0);
                 for (int i = 0; i < w.steps; ++i) {
                     const int t0 = step_token(w, i);
@@ -113,7 +114,7 @@ static void bad_contents(std::mt19937 &rng)
                         for (int cap : {16, 1 << 30})
                             for (int T : {8, 1 << 30}) {
                                 const Span w = span(c0, c1, len, T, cap, 1, block, 64, window,
-                                                    window, 3);
+                                                    window, 3, 4);
                                 if (!w.rows)
                                     continue;
                                 CHECK(c0 >= 0 && (int64_t)c0 + w.rows <= T && w.row0 >= 0 &&
@@ -135,13 +136,15 @@ static void plans()
                     for (int64_t D : {64, 128, 256})
                         for (int64_t len : {1, 64, 300, 4096, 32768, 1 << 30})
                             for (int64_t window : {0, 1, 1000, 1 << 30}) {
-                                const Plan p = plan(T, B, hkv, rep, D, len, window, 1 << 30);
+                                const Plan p = plan(T, B, hkv, rep, D, T % 3 ? D : 32, len, window,
+                                                    1 << 30);
+                                CHECK(p.least >= 1 && (int64_t)p.least * p.splits < 1 << 20, "least");
                                 CHECK(p.splits >= 1 && p.splits <= 128, "splits %d", p.splits);
                                 CHECK(p.rows == 16 || p.rows == 64 || p.rows == 128 || p.rows == 256, "rows");
                                 taken[p.rows == 16 ? 0 : p.rows == 64 ? 1 : p.rows == 128 ? 2 : 3] = true;
                                 cut = cut || p.splits > 1;
                             }
-    CHECK(taken[1] && taken[2] && taken[3] && cut, "a kernel is never taken");
+    CHECK(taken[0] && taken[1] && taken[2] && taken[3] && cut, "a kernel is never taken");
 }
 
 int main()

@@ -246,6 +246,7 @@ def test_workspace_size_of_bad_sizes():
     f = q.quarot_kv_paged_attention_workspace_size
     good = (8, 2, 8, 2, 128, 30000, 0, 0)
     assert f(*good) > 0
+    assert f(8, 2, 8, 2, 128, 30000, group=0) == 0
     for i, bad in ((0, 0), (0, -3), (0, 1 << 62), (1, 0), (1, 1 << 62), (2, 0), (2, 7), (2, 1 << 62),
                    (3, 0), (4, 96), (5, 0), (6, -1), (7, -1)):
         a = list(good)
