@@ -17,6 +17,7 @@
 // outputs are binary32; weights are rounded to fp16 for the product.
 #include <algorithm>
 
+#include "lds_dma.hpp"
 #include "paged.hpp"
 
 namespace quarot {
@@ -66,16 +67,35 @@ __device__ __forceinline__ h2v bits_h2(uint32_t b)
     return __builtin_bit_cast(h2v, b);
 }
 
+// Masks and exponents of the code pairs, in registers: v_and_or_b32 takes no
+// literal, and with constants in sight the compiler splits it into an and and an
+// or, so they pass through an empty asm once.
+struct NibConst {
+    uint32_t mlo, mhi, glo, ghi;
+};
+
+__device__ __forceinline__ NibConst nib_const()
+{
+    NibConst k = {0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
+    __asm__("" : "+s"(k.mlo), "+s"(k.mhi), "+v"(k.glo), "+v"(k.ghi));
+    return k;
+}
+
 // Two codes as fp16 integers: or-ed into the significand of 1024 (where fp16
 // values are spaced by 1) or, for the nibbles at bits 4-7 and 20-23, of 64
 // (spaced by 1/16), minus that.
 template <bool HI>
-__device__ __forceinline__ h2v nib_pair(uint32_t w)
+__device__ __forceinline__ h2v nib_pair(uint32_t w, const NibConst &k)
 {
-    const uint32_t x = HI ? (w & 0x00F000F0u) | 0x54005400u : (w & 0x000F000Fu) | 0x64006400u;
+    const uint32_t x = HI ? (w & k.mhi) | k.ghi : (w & k.mlo) | k.glo;
     const _Float16 b = HI ? (_Float16)-64.0f : (_Float16)-1024.0f;
     const h2v off = {b, b};
     return bits_h2(x) + off;
+}
+
+__device__ __forceinline__ h2v pk_rtz(float a, float b)
+{
+    return __builtin_bit_cast(h2v, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
 __device__ __forceinline__ h2v fma2(h2v a, h2v b, h2v c)
@@ -92,13 +112,13 @@ __device__ __forceinline__ uint4 nib_order(uint4 r)
 }
 
 // The values of a dword of codes (8 elements) in that order.
-__device__ __forceinline__ uint4 unpack8(uint32_t w, h2v s, h2v z)
+__device__ __forceinline__ uint4 unpack8(uint32_t w, h2v s, h2v z, const NibConst &nk)
 {
     const uint32_t w8 = w >> 8;
-    return make_uint4(__builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w8), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w8), s, z)));
+    return make_uint4(__builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w, nk), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w, nk), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w8, nk), s, z)),
+                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w8, nk), s, z)));
 }
 
 __device__ __forceinline__ h2v pair_of(uint32_t lo, uint32_t hi)
@@ -185,7 +205,7 @@ __device__ __forceinline__ void read_ahead(const PagedAttnArgs &a, const Work &w
 }
 
 template <int D, int NT>
-__device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r)
+__device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r, const NibConst &nk)
 {
     using A = Ahead<D, NT>;
 #pragma unroll
@@ -199,7 +219,7 @@ __device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r)
             for (int x = 0; x < 4; ++x)
                 *reinterpret_cast<uint4 *>(st.k + t * (2 * D) +
                                            (((4 * sl + x) ^ (t & Stage<D>::KSW)) * 16)) =
-                    unpack8(w[x], s, z);
+                    unpack8(w[x], s, z, nk);
             if (sl == 0 && (t & 15) == 0)
                 st.ok[t >> 4] = r.ok[i];
         } else if (item < 4 * D) {
@@ -219,8 +239,8 @@ __device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) {
                     const int d = dg * 8 + 2 * bt + hi;
-                    const h2v a01 = hi ? nib_pair<true>(x01) : nib_pair<false>(x01);
-                    const h2v a23 = hi ? nib_pair<true>(x23) : nib_pair<false>(x23);
+                    const h2v a01 = hi ? nib_pair<true>(x01, nk) : nib_pair<false>(x01, nk);
+                    const h2v a23 = hi ? nib_pair<true>(x23, nk) : nib_pair<false>(x23, nk);
                     *reinterpret_cast<uint2 *>(st.v + d * (2 * TT) +
                                                ((unit ^ ((d ^ (d >> 3)) & 7)) * 16) + piece * 8) =
                         make_uint2(__builtin_bit_cast(uint32_t, fma2(a01, s01, z01)),
@@ -296,10 +316,11 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
     const int pw0 = w.pos0 + min(w.row0 + wave * 32, w.rows - 1) / a.rep;
     const int pw1 = w.pos0 + min(w.row0 + wave * 32 + 31, w.rows - 1) / a.rep;
 
+    const NibConst nk = nib_const();
     Ahead<D, NT> ah;
     if (begin < end) {
         read_ahead<D, NT>(a, w, pl.h, token0(begin), ah);
-        put<D, NT>(st[0], ah);
+        put<D, NT>(st[0], ah, nk);
         __syncthreads();
     }
     for (int i = begin; i < end; ++i) {
@@ -380,7 +401,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
             }
         }
         if (i + 1 < end)
-            put<D, NT>(st[(i + 1 - begin) & 1], ah);
+            put<D, NT>(st[(i + 1 - begin) & 1], ah, nk);
         __syncthreads();
     }
 
@@ -427,25 +448,57 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
 // they are, so that nothing of a key or value is rounded:
 //   q . khat_t = ks_t (q . code_t) + kz_t sum(q),
 //   sum_t p_t vhat_t = sum_t (p_t vs_t) code_t + sum_t p_t vz_t.
-// The weights p_t vs_t are two bf16 parts (16 bits; bf16 holds them whatever the
-// values' scale is, where fp16 would lose small ones), each an A operand of its
-// own.  A code c is or-ed into a significand: 64 + c in the K operand (fp16
-// 0x5400, values spaced by 1/16), 128 + c in the V operand (bf16 0x4300, spaced
-// by 1); what the offset adds is taken off in binary32, 64 sum(q) from a score and 128 times the
-// sum of the weights as they were multiplied (a product with ones) from an
-// output: an offset of 64 or 128 costs 6 or 7 of binary32's 24 bits.
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-
-constexpr int ROWS_W = 4;  // waves
+// A code c is or-ed into an fp16 significand: as 64 + c in the K operand, whose
+// offset 64 sum(q) is taken off by the scores' initial accumulator (6 of
+// binary32's 24 bits of scores that are far below it anyway), and as 1024 + c or
+// 64 + c in the V operand, taken off by a packed add: an output over many tokens
+// is small beside the sum of its weights, and offsets of 128 left in the
+// products cost half an fp16 step over 32768 tokens.
+//
+// The weights p_t vs_t are two fp16 parts, an A operand each, 22 bits together
+// while they are above 2^-14.  So the reference m that is taken off the scores x
+// (log2 units) follows the weights and not the scores: it makes the first step's
+// largest weight 1 whatever the values' scale is, and moves when a weight passes
+// 2^15.  (Scales below 2^-24, none but 0 in fp16, count as that, so that rows of
+// equal values have a reference.)
+//
+// A wave's codes and constants come through a ring of its own in LDS, 32 tokens
+// a stage, by loads that go from memory straight there (16 bytes a lane): the
+// next stage is on its way while this one is multiplied, at no registers, and
+// the lanes take each cached row in the pieces that the matrix operands want.
+constexpr int ROWS_W = 4;   // waves of a block
+constexpr int ROWS_NS = 2;  // stages of a wave's ring
 
 template <int D>
-__global__ __launch_bounds__(64 * ROWS_W) void k_paged_rows(PagedAttnArgs a, int slots)
+struct RowsRing {
+    static constexpr int KB = 32 * D / 2;  // bytes of a stage's K codes, and of its V codes
+    static constexpr int STAGE = 2 * KB + 256;  // and ks, kz, vs, vz of 32 tokens
+    static constexpr int LOADS = 2 * (KB / 1024) + 1;
+    static constexpr int UPR = D / 32;  // 16-byte units of a row
+    // K: unit c of row n at c ^ swz(n), so that 16 rows' same unit falls on
+    // different banks
+    __device__ static int swz(int n)
+    {
+        return D == 128 ? (n >> 2) & 3 : D == 256 ? (n >> 1) & 7 : 0;
+    }
+    // V: token 4 g + j of a 16-token group is row 4 j + g, so that the four lane
+    // groups' rows lie side by side
+    __device__ static int token_of(int r)
+    {
+        return 4 * (r & 3) + (r >> 2);
+    }
+};
+
+template <int D>
+__global__ __launch_bounds__(64 * ROWS_W)
+    __attribute__((amdgpu_waves_per_eu(D == 256 ? 2 : 4, D == 256 ? 2 : 4))) void k_paged_rows(PagedAttnArgs a, int slots)
 {
+    using Ring = RowsRing<D>;
     constexpr int MR = paged::FEW_ROWS;
     constexpr int KW = D / 32;  // dwords of K codes of a lane: D / 4 elements of a token
     constexpr int VD = D / 16;  // dimensions of a lane in the value product
-    constexpr float RAISE = 16.0f;  // a maximum moves when a score passes it by 2^16
-    __shared__ float red[ROWS_W][MR][D + 2];
+    constexpr int RED = ROWS_W * MR * (D + 2) * 4, RING = ROWS_W * ROWS_NS * Ring::STAGE;
+    __shared__ __align__(16) uint8_t lds[RED > RING ? RED : RING];
     __shared__ int shb;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 15, g = lane >> 4;
@@ -481,183 +534,253 @@ __global__ __launch_bounds__(64 * ROWS_W) void k_paged_rows(PagedAttnArgs a, int
     }
     const float qs = qsum * c2, q64 = -64.0f * qsum;
 
-    v4f o[VD], o1 = {0.0f, 0.0f, 0.0f, 0.0f};
+    v4f o[VD];
 #pragma unroll
     for (int d = 0; d < VD; ++d)
         o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -inf, l = 0.0f, zs = 0.0f;
 
-    const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
-    for (int i0 = begin + wave; i0 < end; i0 += ROWS_W * 16) {
-        // the pool rows of the next 16 steps' 64 groups of 16 tokens, one a lane
-        int64_t base = -1;
-        {
-            const int i = i0 + (lane >> 2) * ROWS_W;
-            if (i < end) {
-                const int t = paged::step_token(w, i) + 16 * (lane & 3);
+    // this wave's stages: stage k is half k % 2 of step begin + wave + 4 (k / 2)
+    const int begin = pl.split * w.per + wave, end = min(w.steps, pl.split * w.per + w.per);
+    const int stages = begin < end ? 2 * ((end - begin + ROWS_W - 1) / ROWS_W) : 0;
+    auto token_at = [&](int k) {
+        return paged::step_token(w, begin + (k >> 1) * ROWS_W) + 32 * (k & 1);
+    };
+    uint8_t *ring = lds + wave * (ROWS_NS * Ring::STAGE);
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(
+        (uint32_t)reinterpret_cast<uintptr_t>(
+            (__attribute__((address_space(3))) uint8_t *)ring));
+
+    // this lane's source within a 16-token group (a load of K or V codes is 1024
+    // / D * 2 tokens), and its constants' array
+    constexpr int TPL = 2048 / D;  // tokens of a load: 32, 16, 8
+    uint32_t koff[TPL < 16 ? 2 : 1], voff[TPL < 16 ? 2 : 1];
+#pragma unroll
+    for (int x = 0; x < (TPL < 16 ? 2 : 1); ++x) {
+        const int rw = (x * TPL + lane / Ring::UPR) & 15, c = lane % Ring::UPR;
+        koff[x] = rw * (D / 2) + (c ^ Ring::swz(rw)) * 16;
+        voff[x] = Ring::token_of(rw) * (D / 2) + c * 16;
+    }
+    const uint16_t *carr = lane < 16 ? a.kp.s : lane < 32 ? a.kp.z : lane < 48 ? a.vp.s : a.vp.z;
+    carr += (lane & 7) * 2;
+
+    int64_t base = -1;  // pool rows of the next 64 groups of 16 tokens, one a lane
+    auto issue = [&](int k) -> int {
+        if ((k & 31) == 0) {
+            const int kk = k + (lane >> 1);
+            base = -1;
+            if (kk < stages) {
+                const int t = token_at(kk) + 16 * (lane & 1);
                 if (t < w.hi)
                     base = pool_row(a.map, a.hkv, w.b, t);
                 if (base >= 0)
                     base += (int64_t)pl.h * a.map.page;
             }
         }
-#pragma unroll 1
-        for (int j = 0; j < 16 && i0 + j * ROWS_W < end; ++j) {
-            const int t0 = paged::step_token(w, i0 + j * ROWS_W);
-#pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                const int th = t0 + 32 * half;
-                uint32_t kc[2][KW], vc[2][4][(VD + 7) / 8];
-                uint2 ks[2], kz[2], vs[2], vz[2];
-                bool ok[2];
+        int64_t r0[2];
+        int ok = 0;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int src = 4 * j + 2 * half + u;
-                    const uint32_t blo = __builtin_amdgcn_readlane((uint32_t)base, src);
-                    const uint32_t bhi = __builtin_amdgcn_readlane((uint32_t)(base >> 32), src);
-                    const int64_t b0 = (int64_t)(((uint64_t)bhi << 32) | blo);
-                    ok[u] = b0 >= 0;
-                    const int64_t r0 = ok[u] ? b0 : 0;  // a row of the pool, masked below
-                    const uint8_t *kp = a.kp.c + r0 * (D / 2) + (n * (D / 2) + g * (D / 8));
-                    const uint8_t *vp = a.vp.c + r0 * (D / 2) + (4 * g * (D / 2) + n * (D / 32));
-                    __builtin_memcpy(kc[u], __builtin_assume_aligned(kp, D / 8 < 16 ? D / 8 : 16),
-                                     4 * KW);
+        for (int u = 0; u < 2; ++u) {
+            const int src = 2 * (k & 31) + u;
+            const uint32_t blo = __builtin_amdgcn_readlane((uint32_t)base, src);
+            const uint32_t bhi = __builtin_amdgcn_readlane((uint32_t)(base >> 32), src);
+            r0[u] = (int64_t)(((uint64_t)bhi << 32) | blo);
+            ok |= r0[u] >= 0 ? 1 << u : 0;
+            r0[u] = r0[u] >= 0 ? r0[u] : 0;  // a row of the pool, masked where it is used
+        }
+        const uint32_t at = ring_at + (uint32_t)(k % ROWS_NS) * Ring::STAGE;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage's last reads
+        if constexpr (D == 64) {
+            const int64_t rl = (lane >= 32 ? r0[1] : r0[0]) * (D / 2);
+            dma16(a.kp.c + rl + koff[0], at);
+            dma16(a.vp.c + rl + voff[0], at + Ring::KB);
+        } else {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if constexpr (D == 64)
-                            vc[u][t][0] = *reinterpret_cast<const uint16_t *>(vp + t * (D / 2));
-                        else
-                            __builtin_memcpy(vc[u][t], __builtin_assume_aligned(vp + t * (D / 2), D / 32),
-                                             D / 32);
-                    ks[u] = *reinterpret_cast<const uint2 *>(a.kp.s + r0 + 4 * g);
-                    kz[u] = *reinterpret_cast<const uint2 *>(a.kp.z + r0 + 4 * g);
-                    vs[u] = *reinterpret_cast<const uint2 *>(a.vp.s + r0 + 4 * g);
-                    vz[u] = *reinterpret_cast<const uint2 *>(a.vp.z + r0 + 4 * g);
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int x = 0; x < 16 / TPL; ++x) {
+                    dma16s(koff[x], a.kp.c + r0[u] * (D / 2), at + (u * (16 / TPL) + x) * 1024);
+                    dma16s(voff[x], a.vp.c + r0[u] * (D / 2),
+                           at + Ring::KB + (u * (16 / TPL) + x) * 1024);
                 }
-                float x[2][4];
+        }
+        dma4(carr + (lane & 8 ? r0[1] : r0[0]), at + 2 * Ring::KB);
+        return ok;
+    };
+
+    const NibConst nk = nib_const();
+    int ok_next = stages > 0 ? issue(0) : 0;
+    for (int k = 0; k < stages; ++k) {
+        const int ok = ok_next, th = token_at(k);
+        if (k + 1 < stages) {
+            ok_next = issue(k + 1);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Ring::LOADS) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        const uint8_t *stg = ring + (k % ROWS_NS) * Ring::STAGE;
+        const uint8_t *cst = stg + 2 * Ring::KB + 8 * g;  // + 64 array + 32 group
+        float x[2][4];
+        _Float16 ksh[2][4], kzh[2][4], vsh[2][4], vzh[2][4];  // enter v_fma_mix as they are
+        auto halfs = [&](int arr, int u, _Float16 *f) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(cst + 64 * arr + 32 * u);
+            const h2v lo = bits_h2(v.x), hi = bits_h2(v.y);
+            f[0] = lo[0];
+            f[1] = lo[1];
+            f[2] = hi[0];
+            f[3] = hi[1];
+        };
+        const float ms = m > -inf ? m : 0.0f;  // nothing seen so far: weights 0
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    v4f acc = {q64, q64, q64, q64};
+        for (int u = 0; u < 2; ++u) {
+            uint32_t kc[KW];
+            {
+                const uint8_t *kr = stg + u * (Ring::KB / 2) + n * (D / 2);
+                if constexpr (D == 64) {
+                    __builtin_memcpy(kc, __builtin_assume_aligned(kr + 8 * g, 8), 8);
+                } else {
 #pragma unroll
-                    for (int k = 0; k < KW; ++k) {
-                        const uint32_t wd = kc[u][k];
-                        auto f64 = [](uint32_t b) { return (b & 0x00F000F0u) | 0x54005400u; };
-                        const uint4 kf = make_uint4(f64(wd << 4), f64(wd), f64(wd >> 4), f64(wd >> 8));
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, kf), qb[k],
-                                                                     acc, 0, 0, 0);
-                    }
-                    const h2v s01 = bits_h2(ks[u].x), s23 = bits_h2(ks[u].y);
-                    const h2v z01 = bits_h2(kz[u].x), z23 = bits_h2(kz[u].y);
-                    const float sf[4] = {(float)s01[0], (float)s01[1], (float)s23[0], (float)s23[1]};
-                    const float zf[4] = {(float)z01[0], (float)z01[1], (float)z23[0], (float)z23[1]};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        x[u][r] = __builtin_fmaf(sf[r], acc[r] * c2, zf[r] * qs);
-                }
-                if (!(ok[0] & ok[1]) || th + 31 > pmin || (a.window > 0 && th <= pmax - a.window)) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        uint32_t keep[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int t = th + 16 * u + 4 * g + r;
-                            const bool see = ok[u] && t <= p && (t > wfirst || t < a.sinks);
-                            x[u][r] = see ? x[u][r] : -inf;
-                            keep[r] = see ? 0xFFFFu : 0u;
-                        }
-                        // a weight of 0 times what a slot that was never written
-                        // holds may be NaN
-                        const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
-                        vs[u].x &= k01;
-                        vs[u].y &= k23;
-                        vz[u].x &= k01;
-                        vz[u].y &= k23;
-                    }
-                }
-                float mt = x[0][0];
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        mt = fmaxf(mt, x[u][r]);
-                if (__any(mt > m + RAISE)) {  // always where m is -inf and a token is seen
-                    mt = lane_max<4>(mt);
-                    mt = lane_max<5>(mt);
-                    const float mn = fmaxf(m, mt);
-                    const float f = __builtin_amdgcn_exp2f(m - (mn > -inf ? mn : 0.0f));
-                    m = mn;
-                    l *= f;
-                    zs *= f;
-                    float fr[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        fr[r] = __shfl(f, 4 * g + r);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        o1[r] *= fr[r];
-#pragma unroll
-                        for (int d = 0; d < VD; ++d)
-                            o[d][r] *= fr[r];
-                    }
-                }
-                const float ms = m > -inf ? m : 0.0f;
-                uint32_t hh[4], ll[4];  // weights of the 32 tokens, as bf16 pairs
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const h2v s01 = bits_h2(vs[u].x), s23 = bits_h2(vs[u].y);
-                    const h2v z01 = bits_h2(vz[u].x), z23 = bits_h2(vz[u].y);
-                    const float sf[4] = {(float)s01[0], (float)s01[1], (float)s23[0], (float)s23[1]};
-                    const float zf[4] = {(float)z01[0], (float)z01[1], (float)z23[0], (float)z23[1]};
-                    uint32_t wb[4], rb[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float e = __builtin_amdgcn_exp2f(x[u][r] - ms);
-                        l += e;
-                        zs = __builtin_fmaf(e, zf[r], zs);
-                        const float wt = e * sf[r];
-                        wb[r] = __float_as_uint(wt);
-                        rb[r] = __float_as_uint(wt - __uint_as_float(wb[r] & 0xFFFF0000u));
-                    }
-                    hh[2 * u] = perm_b32(wb[1], wb[0], 0x07060302u);
-                    hh[2 * u + 1] = perm_b32(wb[3], wb[2], 0x07060302u);
-                    ll[2 * u] = perm_b32(rb[1], rb[0], 0x07060302u);
-                    ll[2 * u + 1] = perm_b32(rb[3], rb[2], 0x07060302u);
-                }
-                const v8bf wh = __builtin_bit_cast(v8bf, make_uint4(hh[0], hh[1], hh[2], hh[3]));
-                const v8bf wl = __builtin_bit_cast(v8bf, make_uint4(ll[0], ll[1], ll[2], ll[3]));
-                const v8bf ones = __builtin_bit_cast(
-                    v8bf, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
-                o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, ones, o1, 0, 0, 0);
-                o1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, ones, o1, 0, 0, 0);
-#pragma unroll
-                for (int bt = 0; bt < VD / 2; ++bt) {
-                    // byte bt of tokens 4 g, 4 g + 1 (and + 2, + 3) of both groups
-                    const int wd = bt / 4;
-                    const uint32_t sel = (uint32_t)(bt & 3) | 0x0C00u |
-                                         ((uint32_t)(4 + (bt & 3)) << 16) | 0x0C000000u;
-                    uint32_t lo[4], hi[4];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t b2 = perm_b32(vc[u][2 * e + 1][wd], vc[u][2 * e][wd], sel);
-                            lo[2 * u + e] = (b2 & 0x000F000Fu) | 0x43004300u;
-                            hi[2 * u + e] = ((b2 >> 4) & 0x000F000Fu) | 0x43004300u;
-                        }
-                    const v8bf vlo = __builtin_bit_cast(v8bf, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-                    const v8bf vhi = __builtin_bit_cast(v8bf, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-                    o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, vlo, o[2 * bt], 0, 0, 0);
-                    o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, vlo, o[2 * bt], 0, 0, 0);
-                    o[2 * bt + 1] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(wh, vhi, o[2 * bt + 1], 0, 0, 0);
-                    o[2 * bt + 1] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
+                    for (int c = 0; c < KW / 4; ++c)
+                        __builtin_memcpy(kc + 4 * c,
+                                         __builtin_assume_aligned(
+                                             kr + (((KW / 4) * g + c) ^ Ring::swz(n)) * 16, 16), 16);
                 }
             }
+            v4f acc = {q64, q64, q64, q64};
+#pragma unroll
+            for (int c = 0; c < KW; ++c) {
+                const uint32_t wd = kc[c];
+                auto f64 = [&](uint32_t b) { return (b & nk.mhi) | nk.ghi; };
+                const uint4 kf = make_uint4(f64(wd << 4), f64(wd), f64(wd >> 4), f64(wd >> 8));
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, kf), qb[c], acc,
+                                                             0, 0, 0);
+            }
+            halfs(0, u, ksh[u]);
+            halfs(1, u, kzh[u]);
+            halfs(2, u, vsh[u]);
+            halfs(3, u, vzh[u]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                x[u][r] = __builtin_fmaf((float)ksh[u][r], acc[r] * c2,
+                                         __builtin_fmaf((float)kzh[u][r], qs, -ms));
+        }
+        if (ok != 3 || th + 31 > pmin || (a.window > 0 && th <= pmax - a.window)) {
+            asm volatile("");  // a branch, not selects in every step
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = th + 16 * u + 4 * g + r;
+                    const bool see = (ok >> u & 1) && t <= p && (t > wfirst || t < a.sinks);
+                    x[u][r] = see ? x[u][r] : -inf;
+                    // a weight of 0 times what a slot that was never written
+                    // holds may be NaN
+                    vsh[u][r] = see ? vsh[u][r] : (_Float16)0.0f;
+                    vzh[u][r] = see ? vzh[u][r] : (_Float16)0.0f;
+                }
+        }
+        // weights, sums, and whether the reference still does
+        float wt[2][4], ln = l, zn = zs, most = 0.0f;
+        auto weigh = [&]() {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(x[u][r]);
+                    ln += e;
+                    zn = __builtin_fmaf(e, (float)vzh[u][r], zn);
+                    wt[u][r] = __builtin_fmaf(e, (float)vsh[u][r], 0.0f);
+                    most = fmaxf(most, wt[u][r]);
+                }
+        };
+        weigh();
+        // (the sum as well: a value scale of 0 has no weight)
+        if (__any(!(most <= 0x1p15f) || !(ln < 0x1p60f) || m == -inf)) {
+            float y = -inf;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    y = fmaxf(y, x[u][r] + __builtin_amdgcn_logf(fmaxf((float)vsh[u][r], 0x1p-24f)));
+            y = lane_max<4>(y);
+            y = lane_max<5>(y);
+            const float mn = fmaxf(m, ms + y);
+            const float up = (mn > -inf ? mn : 0.0f) - ms;
+            const float f = m > -inf ? __builtin_amdgcn_exp2f(-up) : 0.0f;
+            m = mn;
+            ln = l * f;
+            zn = zs * f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[u][r] -= up;
+            float fr[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                fr[r] = __shfl(f, 4 * g + r);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int d = 0; d < VD; ++d)
+                    o[d][r] *= fr[r];
+            weigh();
+        }
+        l = ln;
+        zs = zn;
+        uint32_t hh[4], ll[4];  // weights of the 32 tokens, as fp16 pairs
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                // the first part truncated, the second what that leaves
+                const h2v hi = pk_rtz(wt[u][r], wt[u][r + 1]);
+                hh[2 * u + r / 2] = __builtin_bit_cast(uint32_t, hi);
+                ll[2 * u + r / 2] = __builtin_bit_cast(
+                    uint32_t, pk_rtz(__builtin_fmaf((float)hi[0], -1.0f, wt[u][r]),
+                                     __builtin_fmaf((float)hi[1], -1.0f, wt[u][r + 1])));
+            }
+        const v8h wh = __builtin_bit_cast(v8h, make_uint4(hh[0], hh[1], hh[2], hh[3]));
+        const v8h wl = __builtin_bit_cast(v8h, make_uint4(ll[0], ll[1], ll[2], ll[3]));
+        uint32_t vc[2][4][(VD + 7) / 8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint8_t *vr = stg + Ring::KB + u * (Ring::KB / 2) + (4 * j + g) * (D / 2) +
+                                    n * (D / 32);
+                if constexpr (D == 64)
+                    vc[u][j][0] = *reinterpret_cast<const uint16_t *>(vr);
+                else
+                    __builtin_memcpy(vc[u][j], __builtin_assume_aligned(vr, D / 32), D / 32);
+            }
+#pragma unroll
+        for (int bt = 0; bt < VD / 2; ++bt) {
+            // byte bt of tokens 4 g, 4 g + 1 (and + 2, + 3) of both groups
+            const int wd = bt / 4;
+            const uint32_t sel =
+                (uint32_t)(bt & 3) | 0x0C00u | ((uint32_t)(4 + (bt & 3)) << 16) | 0x0C000000u;
+            h2v lo[4], hi[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t b2 = perm_b32(vc[u][2 * t + 1][wd], vc[u][2 * t][wd], sel);
+                    lo[2 * u + t] = nib_pair<false>(b2, nk);
+                    hi[2 * u + t] = nib_pair<true>(b2, nk);
+                }
+            const v8h vlo = {lo[0][0], lo[0][1], lo[1][0], lo[1][1],
+                             lo[2][0], lo[2][1], lo[3][0], lo[3][1]};
+            const v8h vhi = {hi[0][0], hi[0][1], hi[1][0], hi[1][1],
+                             hi[2][0], hi[2][1], hi[3][0], hi[3][1]};
+            o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, vlo, o[2 * bt], 0, 0, 0);
+            o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vlo, o[2 * bt], 0, 0, 0);
+            o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, vhi, o[2 * bt + 1], 0, 0, 0);
+            o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
         }
     }
 
-    // each wave's (maximum, sum, output) of its rows in LDS, then one of all
+    // each wave's (reference, sum, output) of its rows in LDS, then one of all
     {
         float2 t = lane_pair_swap<4>(l);
         l = t.x + t.y;
@@ -668,12 +791,14 @@ __global__ __launch_bounds__(64 * ROWS_W) void k_paged_rows(PagedAttnArgs a, int
         t = lane_pair_swap<5>(zs);
         zs = t.x + t.y;
     }
+    __syncthreads();  // every wave is through with its ring
+    float (*red)[MR][D + 2] = reinterpret_cast<float (*)[MR][D + 2]>(lds);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const float z = __shfl(zs, 4 * g + r);
 #pragma unroll
         for (int d = 0; d < VD; ++d)
-            red[wave][4 * g + r][VD * n + d] = __builtin_fmaf(-128.0f, o1[r], o[d][r]) + z;
+            red[wave][4 * g + r][VD * n + d] = o[d][r] + z;
     }
     if (g == 0) {
         red[wave][n][D] = m;

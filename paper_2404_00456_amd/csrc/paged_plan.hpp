@@ -117,8 +117,7 @@ inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int6
     const int64_t steps = (seen + STEP - 1) / STEP;
     if (rows <= FEW_ROWS && G == D) {
         p.rows = FEW_ROWS;
-        const int64_t want = std::max<int64_t>(1, 2048 / (B * hkv));
-        p.least = (int)std::min<int64_t>(32, std::max<int64_t>(4, (steps + want - 1) / want));
+        p.least = (int)std::min<int64_t>(16, std::max<int64_t>(8, steps * B * hkv / 2048));
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((steps + p.least - 1) / p.least, 128));
         return p;
     }
