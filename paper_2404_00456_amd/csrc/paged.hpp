@@ -73,16 +73,15 @@ struct PagedAttnArgs {
     float *part_ml;     // [T * hq, splits, 2]: maximum (in log2 units), sum
 };
 
-// Row (head 0) of position t of sequence b in the pools, or -1: no page.
+// Row (head 0) of position t of sequence b in the pools, or -1: no page.  Without
+// a branch, so that it can be scheduled among other work.
 __device__ __forceinline__ int64_t pool_row(const PagedMap &m, int hkv, int b, int t)
 {
     const int pi = (int)(__umulhi((uint32_t)t, m.div.mul) >> m.div.sh);
-    if (t < 0 || pi >= m.max_pages)
-        return -1;
-    const int page = m.table[(int64_t)b * m.max_pages + pi];
-    if (page < 0 || page >= m.n_pages)
-        return -1;
-    return (int64_t)page * hkv * m.page + (t - pi * m.page);
+    const bool in = t >= 0 && pi < m.max_pages;
+    const int page = m.table[(int64_t)b * m.max_pages + (in ? pi : 0)];
+    const int64_t row = (int64_t)page * ((int64_t)hkv * m.page) + (t - pi * m.page);
+    return in && (uint32_t)page < (uint32_t)m.n_pages ? row : -1;
 }
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);

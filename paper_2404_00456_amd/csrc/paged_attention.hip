@@ -140,112 +140,121 @@ struct Stage {
     int ok[4];  // the page of each 16-token group exists
 };
 
-// What a thread reads of a step ahead of its use.  Items 0 .. 2 D - 1 are 32
-// elements of a key, items 2 D .. 4 D - 1 8 elements of 4 tokens' values.
+// What a thread stages of a step: a step is 2 D items of 32 elements of a key and
+// 2 D items of 8 elements of 4 tokens' values.  With more than 2 D threads the
+// waves part the kinds between them, so that one item a thread is in flight;
+// otherwise each thread has N of both.
 template <int D, int NT>
-struct Ahead {
-    static constexpr int ITEMS = 4 * D;
-    static constexpr int N = (ITEMS + NT - 1) / NT;
-    uint4 c[N];       // codes: a key's 32, or 8 of each of 4 tokens
-    uint32_t sc[N][4];  // key: scale, zero; values: scale pairs, zero pairs
-    int ok[N];
+struct Share {
+    static constexpr bool PART = NT > 2 * D;
+    static constexpr int N = PART ? 1 : 2 * D / NT;
 };
 
-template <int D, int NT>
-__device__ __forceinline__ void read_ahead(const PagedAttnArgs &a, const Work &w, int h, int t0,
-                                           Ahead<D, NT> &r)
+struct Item {
+    int64_t row;   // pool row of the next read (its first token's), or -1
+    int t;         // that token
+    int ok;        // the page of what was read exists
+    uint4 c;       // codes: a key's 32, or 8 of each of 4 tokens
+    uint2 s, z;    // scales and zeros: a key's, or those of the four tokens
+};
+
+template <int D, int NT, bool KEY>
+__device__ __forceinline__ void look_up(const PagedAttnArgs &a, const Work &w, int h, int t0, int i,
+                                        Item &r)
 {
-    using A = Ahead<D, NT>;
-    const int ng = D / a.G;
+    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
+    r.t = t0 + (KEY ? item / (D / 32) : item / (D / 8) * 4);
+    const int64_t row = pool_row(a.map, a.hkv, w.b, r.t);  // the next three too: pages are 16 n
+    r.row = row >= 0 ? row + (int64_t)h * a.map.page : -1;
+}
+
+// Rows of no page are read as row 0 of the pool and take no part: a key by `ok`,
+// values by constants of 0.
+template <int D, int NT, bool KEY, bool ONE>
+__device__ __forceinline__ void read_ahead(const PagedAttnArgs &a, const Work &w, int i, Item &r)
+{
+    const int ng = ONE ? 1 : D / a.G;
+    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
+    r.ok = r.row >= 0;
+    const int64_t row = r.ok ? r.row : 0;
+    if constexpr (KEY) {
+        const int sl = item % (D / 32);
+        const int64_t g = row * ng + (ONE ? 0 : sl * 32 / a.G);
+        r.c = *reinterpret_cast<const uint4 *>(a.kp.c + row * (D / 2) + sl * 16);
+        r.s.x = a.kp.s[g];
+        r.z.x = a.kp.z[g];
+    } else {
+        const int dg = item % (D / 8);
+        const uint8_t *src = a.vp.c + row * (D / 2) + dg * 4;
+        r.c.x = *reinterpret_cast<const uint32_t *>(src);
+        r.c.y = *reinterpret_cast<const uint32_t *>(src + D / 2);
+        r.c.z = *reinterpret_cast<const uint32_t *>(src + D);
+        r.c.w = *reinterpret_cast<const uint32_t *>(src + 3 * (D / 2));
+        if constexpr (ONE) {  // four tokens' constants lie side by side
+            r.s = *reinterpret_cast<const uint2 *>(a.vp.s + row);
+            r.z = *reinterpret_cast<const uint2 *>(a.vp.z + row);
+        } else {
+            uint32_t s[4], z[4];
 #pragma unroll
-    for (int i = 0; i < A::N; ++i) {
-        const int item = threadIdx.x + i * NT;
-        r.ok[i] = 0;
-        r.c[i] = make_uint4(0, 0, 0, 0);
-        r.sc[i][0] = r.sc[i][1] = r.sc[i][2] = r.sc[i][3] = 0;
-        if (item < 2 * D) {
-            const int t = t0 + item / (D / 32), sl = item % (D / 32);
-            int64_t row = pool_row(a.map, a.hkv, w.b, t);
-            if (row >= 0) {
-                row += (int64_t)h * a.map.page;
-                r.ok[i] = 1;
-                r.c[i] = *reinterpret_cast<const uint4 *>(a.kp.c + row * (D / 2) + sl * 16);
-                const int64_t g = row * ng + sl * 32 / a.G;
-                r.sc[i][0] = a.kp.s[g];
-                r.sc[i][1] = a.kp.z[g];
+            for (int x = 0; x < 4; ++x) {
+                const int64_t g = (row + x) * ng + dg * 8 / a.G;
+                s[x] = a.vp.s[g];
+                z[x] = a.vp.z[g];
             }
-        } else if (item < 4 * D) {
-            const int j = item - 2 * D;
-            const int t = t0 + j / (D / 8) * 4, dg = j % (D / 8);
-            int64_t row = pool_row(a.map, a.hkv, w.b, t);  // and the next three: pages are 16 n
-            if (row >= 0) {
-                row += (int64_t)h * a.map.page;
-                r.ok[i] = 1;
-                uint32_t cw[4], s[4], z[4];
+            r.s = make_uint2(s[0] | (s[1] << 16), s[2] | (s[3] << 16));
+            r.z = make_uint2(z[0] | (z[1] << 16), z[2] | (z[3] << 16));
+        }
+        // tokens that no row sees take a weight of 0, and 0 times what a slot
+        // holds that was never written may be NaN
+        if (!(r.ok & (r.t + 4 <= w.hi) & (r.t >= w.low))) {
+            uint32_t keep[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    cw[x] = *reinterpret_cast<const uint32_t *>(a.vp.c + (row + x) * (D / 2) + dg * 4);
-                    const int64_t g = (row + x) * ng + dg * 8 / a.G;
-                    s[x] = a.vp.s[g];
-                    z[x] = a.vp.z[g];
-                    // tokens that no row sees take a weight of 0, and 0 times
-                    // what a slot holds that was never written may be NaN
-                    const bool seen = t + x < w.hi && (t + x >= w.low || t + x < a.sinks);
-                    s[x] = seen ? s[x] : 0;
-                    z[x] = seen ? z[x] : 0;
-                }
-                r.c[i] = make_uint4(cw[0], cw[1], cw[2], cw[3]);
-                r.sc[i][0] = s[0] | (s[1] << 16);
-                r.sc[i][1] = s[2] | (s[3] << 16);
-                r.sc[i][2] = z[0] | (z[1] << 16);
-                r.sc[i][3] = z[2] | (z[3] << 16);
+            for (int x = 0; x < 4; ++x) {
+                const int t = r.t + x;
+                keep[x] = (r.ok & (t < w.hi) & ((t >= w.low) | (t < a.sinks))) ? 0xFFFFu : 0u;
             }
+            const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
+            r.s = make_uint2(r.s.x & k01, r.s.y & k23);
+            r.z = make_uint2(r.z.x & k01, r.z.y & k23);
         }
     }
 }
 
-template <int D, int NT>
-__device__ __forceinline__ void put(Stage<D> &st, const Ahead<D, NT> &r, const NibConst &nk)
+template <int D, int NT, bool KEY>
+__device__ __forceinline__ void put(Stage<D> &st, int i, const Item &r, const NibConst &nk)
 {
-    using A = Ahead<D, NT>;
+    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
+    if constexpr (KEY) {
+        const int t = item / (D / 32), sl = item % (D / 32);
+        const h2v s = bits_h2(perm_b32(r.s.x, r.s.x, 0x01000100u));
+        const h2v z = bits_h2(perm_b32(r.z.x, r.z.x, 0x01000100u));
+        const uint32_t w[4] = {r.c.x, r.c.y, r.c.z, r.c.w};
 #pragma unroll
-    for (int i = 0; i < A::N; ++i) {
-        const int item = threadIdx.x + i * NT;
-        if (item < 2 * D) {
-            const int t = item / (D / 32), sl = item % (D / 32);
-            const h2v s = pair_of(r.sc[i][0], r.sc[i][0]), z = pair_of(r.sc[i][1], r.sc[i][1]);
-            const uint32_t w[4] = {r.c[i].x, r.c[i].y, r.c[i].z, r.c[i].w};
+        for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<uint4 *>(st.k + t * (2 * D) + (((4 * sl + x) ^ (t & Stage<D>::KSW)) * 16)) =
+                unpack8(w[x], s, z, nk);
+        st.ok[t >> 4] = r.ok;  // (every lane of a 16-token group writes the same)
+    } else {
+        const int q = item / (D / 8), dg = item % (D / 8);
+        // tokens 4 q .. 4 q + 3: 16-token group q / 4, lane half q % 2, 8-byte
+        // piece (q / 2) % 2
+        const int unit = (q >> 2) * 2 + (q & 1), piece = (q >> 1) & 1;
+        const h2v s01 = bits_h2(r.s.x), s23 = bits_h2(r.s.y);
+        const h2v z01 = bits_h2(r.z.x), z23 = bits_h2(r.z.y);
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                *reinterpret_cast<uint4 *>(st.k + t * (2 * D) +
-                                           (((4 * sl + x) ^ (t & Stage<D>::KSW)) * 16)) =
-                    unpack8(w[x], s, z, nk);
-            if (sl == 0 && (t & 15) == 0)
-                st.ok[t >> 4] = r.ok[i];
-        } else if (item < 4 * D) {
-            const int j = item - 2 * D;
-            const int q = j / (D / 8), dg = j % (D / 8);
-            // tokens 4 q .. 4 q + 3: 16-token group q / 4, lane half q % 2,
-            // 8-byte piece (q / 2) % 2
-            const int unit = (q >> 2) * 2 + (q & 1), piece = (q >> 1) & 1;
-            const h2v s01 = bits_h2(r.sc[i][0]), s23 = bits_h2(r.sc[i][1]);
-            const h2v z01 = bits_h2(r.sc[i][2]), z23 = bits_h2(r.sc[i][3]);
+        for (int bt = 0; bt < 4; ++bt) {
+            // byte bt of two tokens in bytes 0 and 2
+            const uint32_t sel = (uint32_t)bt | 0x0C00u | ((uint32_t)(4 + bt) << 16) | 0x0C000000u;
+            const uint32_t x01 = perm_b32(r.c.y, r.c.x, sel), x23 = perm_b32(r.c.w, r.c.z, sel);
 #pragma unroll
-            for (int bt = 0; bt < 4; ++bt) {
-                // byte bt of two tokens in bytes 0 and 2
-                const uint32_t sel = (uint32_t)bt | 0x0C00u | ((uint32_t)(4 + bt) << 16) | 0x0C000000u;
-                const uint32_t x01 = perm_b32(r.c[i].y, r.c[i].x, sel);
-                const uint32_t x23 = perm_b32(r.c[i].w, r.c[i].z, sel);
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi) {
-                    const int d = dg * 8 + 2 * bt + hi;
-                    const h2v a01 = hi ? nib_pair<true>(x01, nk) : nib_pair<false>(x01, nk);
-                    const h2v a23 = hi ? nib_pair<true>(x23, nk) : nib_pair<false>(x23, nk);
-                    *reinterpret_cast<uint2 *>(st.v + d * (2 * TT) +
-                                               ((unit ^ ((d ^ (d >> 3)) & 7)) * 16) + piece * 8) =
-                        make_uint2(__builtin_bit_cast(uint32_t, fma2(a01, s01, z01)),
-                                   __builtin_bit_cast(uint32_t, fma2(a23, s23, z23)));
-                }
+            for (int hi = 0; hi < 2; ++hi) {
+                const int d = dg * 8 + 2 * bt + hi;
+                const h2v a01 = hi ? nib_pair<true>(x01, nk) : nib_pair<false>(x01, nk);
+                const h2v a23 = hi ? nib_pair<true>(x23, nk) : nib_pair<false>(x23, nk);
+                *reinterpret_cast<uint2 *>(st.v + d * (2 * TT) + ((unit ^ ((d ^ (d >> 3)) & 7)) * 16) +
+                                           piece * 8) =
+                    make_uint2(__builtin_bit_cast(uint32_t, fma2(a01, s01, z01)),
+                               __builtin_bit_cast(uint32_t, fma2(a23, s23, z23)));
             }
         }
     }
@@ -269,12 +278,36 @@ __device__ __forceinline__ Place place(const PagedAttnArgs &a, int slots)
     return p;
 }
 
-template <int D, int NW>
+// Orders within a step, for the scheduler: what a wave issues runs in order, so
+// matrix products and vector instructions overlap only where they alternate.
+__device__ __forceinline__ void mix_softmax()
+{
+#if 0
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+#endif
+}
+
+__device__ __forceinline__ void mix_stage()
+{
+}
+
+template <int D, int NW, bool ONE>
 __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slots)
 {
     constexpr int NT = 64 * NW, MR = 32 * NW;
     constexpr int KS = D / 16, DB = D / 32;
-    __shared__ __align__(16) Stage<D> st[2];
+    // stages: one that is multiplied, the next one, and one that is written while
+    // some wave may still be at the first (two, and a barrier more, where three
+    // do not fit)
+    constexpr int NB = D == 256 ? 2 : 3;
+    __shared__ __align__(16) Stage<D> st[NB];
     __shared__ int shb;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, hf = lane >> 5;
@@ -311,98 +344,171 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
     float m = -inf, l = 0.0f;  // in log2 units; this lane's half of the sum
 
     const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
-    auto token0 = [&](int i) { return paged::step_token(w, i); };
-    // the wave's smallest and largest position, for the steps that need no mask
-    const int pw0 = w.pos0 + min(w.row0 + wave * 32, w.rows - 1) / a.rep;
-    const int pw1 = w.pos0 + min(w.row0 + wave * 32 + 31, w.rows - 1) / a.rep;
+    auto token0 = [&](int i) { return paged::step_token(w, i < end ? i : end - 1); };
+    const int pmin = w.pos0 + w.row0 / a.rep, pmax = w.pos0 + (min(w.row0 + MR, w.rows) - 1) / a.rep;
 
-    const NibConst nk = nib_const();
-    Ahead<D, NT> ah;
-    if (begin < end) {
-        read_ahead<D, NT>(a, w, pl.h, token0(begin), ah);
-        put<D, NT>(st[0], ah, nk);
-        __syncthreads();
-    }
-    for (int i = begin; i < end; ++i) {
-        const Stage<D> &cur = st[(i - begin) & 1];
-        const int t0 = token0(i);
-        if (i + 1 < end)
-            read_ahead<D, NT>(a, w, pl.h, token0(i + 1), ah);
-
-        // scores of 64 tokens: registers 8 x + r of s[u] hold token
-        // 32 u + 16 x + 8 (r / 4) + 4 hf + r % 4
-        v16f s[2];
+    // scores of the 32 tokens of half u: register r holds token
+    // 32 u + 8 (r / 4) + 4 hf + r % 4
+    auto score = [&](const Stage<D> &sg, int u) {
+        v16f s;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int r = 0; r < 16; ++r)
+            s[r] = 0.0f;
+        const int t = 32 * u + n;
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[u][r] = 0.0f;
-            const int t = 32 * u + n;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const v8h kf = *reinterpret_cast<const v8h *>(
-                    cur.k + t * (2 * D) + (((2 * k + hf) ^ (t & Stage<D>::KSW)) * 16));
-                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qb[k], s[u], 0, 0, 0);
-            }
+        for (int k = 0; k < KS; ++k) {
+            const v8h kf = *reinterpret_cast<const v8h *>(
+                sg.k + t * (2 * D) + (((2 * k + hf) ^ (t & Stage<D>::KSW)) * 16));
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qb[k], s, 0, 0, 0);
         }
-        const bool all = cur.ok[0] & cur.ok[1] & cur.ok[2] & cur.ok[3];
-        if (!all || t0 + TT - 1 > pw0 || (a.window > 0 && t0 <= pw1 - a.window)) {
+        return s;
+    };
+    // their weights as the value product's B operands, and the sums
+    auto weigh = [&](const v16f &s, v8h *pb, float ms) {
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int t = t0 + 32 * u + 8 * (r >> 2) + 4 * hf + (r & 3);
-                    const bool see = t <= p && (t > wfirst || t < a.sinks) && cur.ok[2 * u + (r >> 3)];
-                    s[u][r] = see ? s[u][r] : -inf;
-                }
+        for (int r = 0; r < 16; ++r) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -ms));
+            sum[r & 3] += e;
+            pb[r >> 3][r & 7] = (_Float16)e;
         }
-        float mt = s[0][0];
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    auto hide = [&](v16f &s, int t0, const int *ok, int u) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int r = 0; r < 16; ++r) {
+            const int t = t0 + 32 * u + 8 * (r >> 2) + 4 * hf + (r & 3);
+            const bool see = (t <= p) & ((t > wfirst) | (t < a.sinks)) & (ok[2 * u + (r >> 3)] != 0);
+            s[r] = see ? s[r] : -inf;
+        }
+    };
+    // takes the weights' sum; where they pass what fp16 holds, or there is no
+    // reference yet, the reference moves to the largest score
+    auto settle = [&](const v16f &s, v8h *pb, float ls) {
+        if (__builtin_expect(__any(!(ls <= 0x1p15f) | (m == -inf)), 0)) {
+            float mt = s[0];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                mt = fmaxf(mt, s[u][r]);
-        {
+            for (int r = 1; r < 16; ++r)
+                mt = fmaxf(mt, s[r]);
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt),
                                                              false, false);
-            mt = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-        }
-        const float mn = fmaxf(m, mt * c2);
-        const float ms = mn > -inf ? mn : 0.0f;  // nothing seen so far: weights 0
-        if (__any(mn > m)) {
-            const float f = __builtin_amdgcn_exp2f(m - ms);  // 0 on the first step
+            const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2);
+            const float ms = mn > -inf ? mn : 0.0f;  // nothing seen so far: weights 0
+            const float f = m > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.0f;
+            m = mn;
             l *= f;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
+                for (int r = 0; r < 16; ++r) {
                     o[d][r] *= f;
-            m = mn;
+                    asm volatile("" : "+v"(o[d]));
+                }
+            ls = weigh(s, pb, ms);
         }
+        l += ls;
+    };
+    auto add_values = [&](const Stage<D> &sg, int u, const v8h *pb) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int x = 0; x < 2; ++x) {
+            const int unit = (2 * u + x) * 2 + hf;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                v8h pb;
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * x + r], c2, -ms));
-                    l += e;
-                    pb[r] = (_Float16)e;
-                }
-                const int unit = (2 * u + x) * 2 + hf;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int dim = 32 * d + n;
-                    const v8h vf = *reinterpret_cast<const v8h *>(
-                        cur.v + dim * (2 * TT) + ((unit ^ ((dim ^ (dim >> 3)) & 7)) * 16));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pb, o[d], 0, 0, 0);
-                }
+            for (int d = 0; d < DB; ++d) {
+                const int dim = 32 * d + n;
+                const v8h vf = *reinterpret_cast<const v8h *>(
+                    sg.v + dim * (2 * TT) + ((unit ^ ((dim ^ (dim >> 3)) & 7)) * 16));
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pb[x], o[d], 0, 0, 0);
             }
         }
-        if (i + 1 < end)
-            put<D, NT>(st[(i + 1 - begin) & 1], ah, nk);
+    };
+
+    if (begin < end) {
+        using Sh = Share<D, NT>;
+        const NibConst nk = nib_const();
+        // 0: this wave stages keys, 1: values, 2: nothing
+        const int role = Sh::PART ? __builtin_amdgcn_readfirstlane(tid / (2 * D)) : 0;
+        Item kv[Sh::PART ? 1 : 2][Sh::N];
+        // f(a kind of item, its items) for what this wave stages, then once `also`
+        auto each = [&](auto f, auto also) {
+            if constexpr (Sh::PART) {
+                if (role == 0) {
+                    f(std::true_type(), kv[0]);
+                    also();
+                } else if (NT <= 4 * D || role == 1) {
+                    f(std::false_type(), kv[0]);
+                    also();
+                } else {
+                    also();
+                }
+            } else {
+                f(std::true_type(), kv[0]);
+                f(std::false_type(), kv[1]);
+                also();
+            }
+        };
+        auto look = [&](int step) {
+            return [&, step](auto key, Item *r) {
+#pragma unroll
+                for (int i = 0; i < Sh::N; ++i)
+                    look_up<D, NT, decltype(key)::value>(a, w, pl.h, token0(step), i, r[i]);
+            };
+        };
+        auto read = [&](auto key, Item *r) {
+#pragma unroll
+            for (int i = 0; i < Sh::N; ++i)
+                read_ahead<D, NT, decltype(key)::value, ONE>(a, w, i, r[i]);
+        };
+        auto write = [&](Stage<D> &to) {
+            return [&](auto key, Item *r) {
+#pragma unroll
+                for (int i = 0; i < Sh::N; ++i)
+                    put<D, NT, decltype(key)::value>(to, i, r[i], nk);
+            };
+        };
+        auto nothing = [] {};
+        each(look(begin), nothing);
+        each(read, nothing);
+        each(write(st[0]), nothing);
+        each(look(begin + 1), nothing);
+        each(read, nothing);
+        each(look(begin + 2), nothing);
         __syncthreads();
+        v16f s0 = score(st[0], 0), s1;
+        int cur = 0;
+        for (int i = begin; i < end; ++i) {
+            const int t0 = token0(i);
+            const Stage<D> &sc = st[cur];
+            const int nx = cur + 1 < NB ? cur + 1 : 0;
+            const int ok[4] = {sc.ok[0], sc.ok[1], sc.ok[2], sc.ok[3]};
+            const bool edge = !(ok[0] & ok[1] & ok[2] & ok[3]) || t0 + TT - 1 > pmin ||
+                              (a.window > 0 && t0 <= pmax - a.window);
+            v8h pb[2];
+            if (edge)
+                hide(s0, t0, ok, 0);
+            s1 = score(sc, 1);
+            float ls = weigh(s0, pb, m > -inf ? m : 0.0f);
+            mix_softmax();
+            settle(s0, pb, ls);
+            each(
+                [&](auto key, Item *r) {
+                    write(st[nx])(key, r);
+                    read(key, r);
+                    look(i + 3)(key, r);
+                },
+                nothing);
+            add_values(sc, 0, pb);
+            if (edge)
+                hide(s1, t0, ok, 1);
+            __syncthreads();  // the next step's stage is whole
+            s0 = score(st[nx], 0);
+            ls = weigh(s1, pb, m > -inf ? m : 0.0f);
+            mix_softmax();
+            settle(s1, pb, ls);
+            add_values(sc, 1, pb);
+            if constexpr (NB == 2)
+                __syncthreads();  // this one may be overwritten
+            cur = nx;
+        }
     }
 
     {
@@ -921,7 +1027,10 @@ hipError_t go_tile(const PagedAttnArgs &a, hipStream_t s)
     constexpr int MR = 32 * NW;
     const int slots = (int)paged::slots(a.map.T, a.map.B, a.rep, MR);
     const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
-    hipLaunchKernelGGL((k_paged_tile<D, NW>), grid, dim3(64 * NW), 0, s, a, slots);
+    if (a.G == D)
+        hipLaunchKernelGGL((k_paged_tile<D, NW, true>), grid, dim3(64 * NW), 0, s, a, slots);
+    else
+        hipLaunchKernelGGL((k_paged_tile<D, NW, false>), grid, dim3(64 * NW), 0, s, a, slots);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1)
         return e;
