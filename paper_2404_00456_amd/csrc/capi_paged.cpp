@@ -98,9 +98,15 @@ void fill_cache(const quarot_paged_kv *c, int64_t T, PagedPool &k, PagedPool &v,
     m.div = paged::divisor(m.page);
 }
 
-size_t attention_workspace(const paged::Plan &p, int64_t T, int64_t n_heads, int64_t head_dim)
+// The launches of a plan use the workspace one after the other.
+size_t attention_workspace(const paged::Plan &p, int64_t T, int64_t batch, int64_t hkv, int64_t rep,
+                           int64_t head_dim)
 {
-    return p.splits > 1 ? (size_t)T * n_heads * p.splits * (size_t)(head_dim + 2) * sizeof(float) : 0;
+    size_t need = 0;
+    for (int i = 0; i < p.n; ++i)
+        need = std::max(need, (size_t)(paged::part_rows(p.part[i], T, batch, rep) * hkv * p.part[i].splits) *
+                                  (size_t)(head_dim + 2) * sizeof(float));
+    return need;
 }
 
 }  // namespace
@@ -215,7 +221,7 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
     const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim, group,
                                    std::min(max_seq_len, kMaxTokens), std::min(window, kMaxTokens),
                                    std::min(n_sinks, kMaxTokens));
-    return attention_workspace(p, T, n_heads, head_dim);
+    return attention_workspace(p, T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim);
 }
 
 quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, quarot_f16 *out,
@@ -245,13 +251,14 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
         return QUAROT_ERR_ALIGNMENT;
     window = std::min(window, kMaxTokens);
     n_sinks = std::min(n_sinks, kMaxTokens);
-    const paged::Plan p = paged::plan(T, cache->batch, cache->n_kv_heads, n_heads / cache->n_kv_heads,
-                                   D, cache->group, std::min(max_seq_len, kMaxTokens), window, n_sinks);
-    // a launch holds fewer than 2^32 threads
-    const int64_t slots = paged::slots(T, cache->batch, n_heads / cache->n_kv_heads, p.rows);
-    if (slots * cache->n_kv_heads * p.splits > 0xFFFFFFFFll / paged::MAX_THREADS)
-        return QUAROT_ERR_UNSUPPORTED_SIZE;
-    const size_t need = attention_workspace(p, T, n_heads, D);
+    const int64_t hkv = cache->n_kv_heads, rep = n_heads / hkv;
+    const paged::Plan p = paged::plan(T, cache->batch, hkv, rep, D, cache->group,
+                                      std::min(max_seq_len, kMaxTokens), window, n_sinks);
+    for (int i = 0; i < p.n; ++i)  // a launch holds fewer than 2^32 threads
+        if (paged::slots(p.part[i], T, cache->batch, rep) * hkv * p.part[i].splits >
+            0xFFFFFFFFll / paged::MAX_THREADS)
+            return QUAROT_ERR_UNSUPPORTED_SIZE;
+    const size_t need = attention_workspace(p, T, cache->batch, hkv, rep, D);
     if (need && (!workspace || workspace_bytes < need))
         return QUAROT_ERR_WORKSPACE;
     if (need && !aligned16(workspace))
@@ -265,18 +272,23 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
     a.out_stride = out_stride;
     fill_cache(cache, T, a.kp, a.vp, a.map);
     a.hq = (int)n_heads;
-    a.hkv = (int)cache->n_kv_heads;
-    a.rep = (int)(n_heads / cache->n_kv_heads);
+    a.hkv = (int)hkv;
+    a.rep = (int)rep;
     a.D = (int)D;
     a.G = (int)cache->group;
     a.window = (int)window;
     a.sinks = (int)n_sinks;
     a.sm_scale = sm_scale;
-    a.splits = p.splits;
-    a.least = p.least;
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = a.part_o + (size_t)T * n_heads * p.splits * D;
-    hipError_t e = launch_paged_attention(a, p, (hipStream_t)stream);
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < p.n && e == hipSuccess; ++i) {
+        const paged::Part &part = p.part[i];
+        a.which = part.which;
+        a.splits = part.splits;
+        a.least = part.least;
+        a.part_o = static_cast<float *>(workspace);
+        a.part_ml = a.part_o + (size_t)(paged::part_rows(part, T, cache->batch, rep) * hkv * part.splits * D);
+        e = launch_paged_attention(a, part.rows, (hipStream_t)stream);
+    }
     return e == hipSuccess ? QUAROT_OK : hip_fail(e);
 }
 

@@ -68,9 +68,10 @@ struct PagedAttnArgs {
     int D, G;
     int window, sinks;  // window 0: none
     float sm_scale;
-    int splits, least;  // of paged::Plan
-    float *part_o;      // [T * hq, splits, D]
-    float *part_ml;     // [T * hq, splits, 2]: maximum (in log2 units), sum
+    paged::Which which;  // of paged::Part
+    int splits, least;
+    float *part_o;       // [rows, hkv, splits, D], rows from paged::part_row on
+    float *part_ml;      // [rows, hkv, splits, 2]: maximum (in log2 units), sum
 };
 
 // Row (head 0) of position t of sequence b in the pools, or -1: no page.  Without
@@ -85,6 +86,6 @@ __device__ __forceinline__ int64_t pool_row(const PagedMap &m, int hkv, int b, i
 }
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
-hipError_t launch_paged_attention(const PagedAttnArgs &a, const paged::Plan &p, hipStream_t s);
+hipError_t launch_paged_attention(const PagedAttnArgs &a, int rows, hipStream_t s);
 
 }  // namespace quarot

@@ -29,7 +29,6 @@ typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
-constexpr int TT = paged::STEP;
 
 // What a block of MR query rows works on.
 struct Work : paged::Span {
@@ -37,29 +36,56 @@ struct Work : paged::Span {
     int tok0;  // first batch row (new token) of the sequence
 };
 
+// Each wave looks for its sequence by itself: a 64-way search of cu (one load's
+// latency up to 64 sequences, two up to 4096), then that sequence's entries from
+// the lanes that hold them.
 template <int MR>
-__device__ __forceinline__ Work find_work(const PagedAttnArgs &a, int slot, int *sh)
+__device__ __forceinline__ Work find_work(const PagedAttnArgs &a, int slot)
 {
     const PagedMap &m = a.map;
-    if (threadIdx.x == 0)
-        *sh = -1;
-    __syncthreads();
-    for (int b = threadIdx.x; b < m.B; b += blockDim.x)
-        if (paged::first_slot((int64_t)m.cu[b] * a.rep, b, MR) <= slot &&
-            slot < paged::first_slot((int64_t)m.cu[b + 1] * a.rep, b + 1, MR))
-            *sh = b;
-    __syncthreads();
+    const int lane = threadIdx.x & 63;
     Work w = {};
-    w.b = __builtin_amdgcn_readfirstlane(*sh);
-    if (w.b < 0)
+    if (a.which == paged::FEW) {
+        w.b = slot;
+        w.tok0 = m.cu[slot];
+        const int c1 = m.cu[slot + 1];
+        if (((int64_t)c1 - w.tok0) * a.rep <= paged::FEW_ROWS)
+            static_cast<paged::Span &>(w) =
+                paged::span(w.tok0, c1, m.len[slot], m.T, m.max_pages * m.page, a.rep, 0, MR,
+                            a.window, a.sinks, a.splits, a.least);
         return w;
-    const int c0 = m.cu[w.b], c1 = m.cu[w.b + 1];
-    static_cast<paged::Span &>(w) =
-        paged::span(c0, c1, m.len[w.b], m.T, m.max_pages * m.page, a.rep,
-                    slot - paged::first_slot((int64_t)c0 * a.rep, w.b, MR), MR, a.window, a.sinks,
-                    a.splits, a.least);
-    w.tok0 = c0;
+    }
+    int lo = 0, n = m.B;
+    while (n > 64) {
+        const int step = (n + 63) / 64, b = lo + min(lane * step, n - 1);
+        const uint64_t below =
+            __ballot(lane * step < n && paged::first_slot((int64_t)m.cu[b] * a.rep, b, MR) <= slot);
+        const int i = below ? 63 - __builtin_clzll(below) : 0;
+        lo += i * step;
+        n = min(step, n - i * step);
+    }
+    const int b = lo + min(lane, n - 1);
+    const int c0 = m.cu[b], c1 = m.cu[b + 1], len = m.len[b];
+    const uint64_t mine = __ballot(paged::first_slot((int64_t)c0 * a.rep, b, MR) <= slot &&
+                                   slot < paged::first_slot((int64_t)c1 * a.rep, b + 1, MR));
+    if (mine == 0)
+        return w;
+    const int i = __builtin_ctzll(mine);
+    w.b = lo + i;
+    w.tok0 = __builtin_amdgcn_readlane(c0, i);
+    static_cast<paged::Span &>(w) = paged::span(
+        w.tok0, __builtin_amdgcn_readlane(c1, i), __builtin_amdgcn_readlane(len, i), m.T,
+        m.max_pages * m.page, a.rep, slot - paged::first_slot((int64_t)w.tok0 * a.rep, w.b, MR), MR,
+        a.window, a.sinks, a.splits, a.least);
+    if (a.which == paged::MANY && w.rows <= paged::FEW_ROWS)
+        w.rows = 0;
     return w;
+}
+
+// First partial result of a row.
+__device__ __forceinline__ int64_t part_of(const PagedAttnArgs &a, const Work &w, int row, int h)
+{
+    return ((paged::part_row(a.which, w.b, w.tok0, a.rep) + row) * a.hkv + h) * a.splits;
 }
 
 __device__ __forceinline__ h2v bits_h2(uint32_t b)
@@ -111,154 +137,229 @@ __device__ __forceinline__ uint4 nib_order(uint4 r)
                       perm_b32(r.w, r.y, 0x05040100u), perm_b32(r.w, r.y, 0x07060302u));
 }
 
-// The values of a dword of codes (8 elements) in that order.
-__device__ __forceinline__ uint4 unpack8(uint32_t w, h2v s, h2v z, const NibConst &nk)
-{
-    const uint32_t w8 = w >> 8;
-    return make_uint4(__builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w, nk), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w, nk), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<false>(w8, nk), s, z)),
-                      __builtin_bit_cast(uint32_t, fma2(nib_pair<true>(w8, nk), s, z)));
-}
-
-__device__ __forceinline__ h2v pair_of(uint32_t lo, uint32_t hi)
-{
-    return bits_h2(lo | (hi << 16));
-}
-
-// Token block i of a step: K as fp16 rows [64][D], the 16-byte unit u of row t
-// at u ^ (t & swizzle); V transposed, [D][64] with the tokens of a 16-token
-// group in the order that the scores' registers have (4 h + r, then 8 + 4 h +
-// r, for lane half h), the 16-byte unit u of dimension d at u ^ ((d ^ d / 8) &
-// 7).  Both swizzles spread the writes and the reads over the banks.
-template <int D>
+// TS tokens in LDS.  K as fp16 rows [TS][D], with 16 bytes of padding, so that 16
+// rows' same 16-byte unit falls on different banks and every address of a lane is
+// one of its own and a constant.  V transposed, [D][TS], a dimension's tokens in
+// the order that the scores' registers have (of a 16-token group 4 h + r, then
+// 8 + 4 h + r, for lane half h: unit 2 group + h).  Rows of V change places in
+// pairs and units within their row, so that neither the reads (16 bytes of
+// neighbouring dimensions) nor the writes (8 bytes of every DV-th) meet on a bank;
+// from one block of 32 dimensions to the next the units' order changes by one bit,
+// so that two addresses of a lane do for all of them.
+template <int D, int TS>
 struct Stage {
-    static constexpr int K_BYTES = TT * D * 2, V_BYTES = TT * D * 2;
-    static constexpr int KSW = D == 64 ? 7 : 15;
-    uint8_t k[K_BYTES];
-    uint8_t v[V_BYTES];
-    int ok[4];  // the page of each 16-token group exists
+    static constexpr int KP = 2 * D + 16, VP = 2 * TS;  // row pitches
+    uint8_t k[TS * KP];
+    uint8_t v[D * VP];
+    int ok[TS / 16];  // the page of each 16-token group exists
+
+    __device__ static int vrow(int d)
+    {
+        return (d ^ (((d >> 2) ^ (d >> 3)) & 1)) * VP;
+    }
+    __device__ static int vunit(int d, int u)
+    {
+        return (u ^ ((((d >> 1) & 7) ^ ((d >> 4) & 3)) & (TS / 8 - 1))) * 16;
+    }
 };
 
-// What a thread stages of a step: a step is 2 D items of 32 elements of a key and
-// 2 D items of 8 elements of 4 tokens' values.  With more than 2 D threads the
-// waves part the kinds between them, so that one item a thread is in flight;
-// otherwise each thread has N of both.
-template <int D, int NT>
+// What a thread stages of TS tokens: N items of EK elements of a key, and N items
+// of DV elements of four tokens' values.  Every thread has some of both, so that
+// no step carries a branch, and the items come to pieces of a pair of values each,
+// which the main loop spreads between its matrix products.  The items of a wave
+// lie in one 16-token group, which is one page's: where it is read from is the
+// same for all lanes, and is kept and worked out in scalar registers.
+template <int D, int TS, int NT>
 struct Share {
-    static constexpr bool PART = NT > 2 * D;
-    static constexpr int N = PART ? 1 : 2 * D / NT;
+    static constexpr int ALL = TS * D / NT;  // elements of a thread
+    static constexpr int EK = std::min({ALL, D / 4, 32}), DV = std::min({ALL / 4, D / 16, 8});
+    static constexpr int N = ALL / EK;
+    static constexpr int PAIRS = N * EK / 2;  // and of the values, N * DV * 2 as many
+    static_assert(N * DV * 4 == ALL && N * EK == ALL, "items cover the tokens");
+    static constexpr int KL = D / EK, VL = D / DV;  // items of a token, of four tokens
+    static_assert(KL >= 4 && VL >= 16, "a wave's items lie in one 16-token group");
 };
 
-struct Item {
-    int64_t row;   // pool row of the next read (its first token's), or -1
-    int t;         // that token
-    int ok;        // the page of what was read exists
-    uint4 c;       // codes: a key's 32, or 8 of each of 4 tokens
-    uint2 s, z;    // scales and zeros: a key's, or those of the four tokens
-};
+template <int D, int TS, int NT, bool ONE>
+struct Ahead {
+    using S = Share<D, TS, NT>;
+    using St = Stage<D, TS>;
+    const PagedAttnArgs &a;
+    const Work &w;
+    int h, wave, lane;
+    int64_t krow[S::N], vrow[S::N];  // pool rows of the groups of the next read, or -1
+    int vt[S::N];                    // first token of the values' group
+    uint32_t kc[S::N][S::EK / 8];    // codes
+    uint32_t vc[S::N][4];
+    uint32_t ks[S::N], kz[S::N];     // constants: a key's, and those of four tokens
+    uint2 vs[S::N], vz[S::N];
+    int kok[S::N];                   // the page of the key that was read exists
 
-template <int D, int NT, bool KEY>
-__device__ __forceinline__ void look_up(const PagedAttnArgs &a, const Work &w, int h, int t0, int i,
-                                        Item &r)
-{
-    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
-    r.t = t0 + (KEY ? item / (D / 32) : item / (D / 8) * 4);
-    const int64_t row = pool_row(a.map, a.hkv, w.b, r.t);  // the next three too: pages are 16 n
-    r.row = row >= 0 ? row + (int64_t)h * a.map.page : -1;
-}
+    // A key item: token ktok of the stage, element ke on.
+    __device__ int kitem(int i) const
+    {
+        return i * NT + wave * 64 + lane;
+    }
+    __device__ int ktok(int i) const
+    {
+        return kitem(i) / S::KL;
+    }
+    // Element of its dword wd of codes: neighbouring lanes' units side by side
+    // where a row is one group.
+    __device__ int ke(int i, int wd) const
+    {
+        const int s = kitem(i) % S::KL;
+        return ONE ? (s + wd * S::KL) * 8 : s * S::EK + wd * 8;
+    }
+    // A values item: quad vq of the tokens of group vgroup, dimension vd on.  A
+    // wave has 16 runs of dimensions of four quads, dealt to the lanes so that 16
+    // of them write to all banks.
+    __device__ int vblock(int i) const
+    {
+        return i * (NT / 64) + wave;
+    }
+    __device__ int vgroup(int i) const
+    {
+        return vblock(i) / (S::VL / 16);
+    }
+    __device__ int vq() const
+    {
+        return (lane >> 5) | (lane >> 2 & 2);
+    }
+    __device__ int vd(int i) const
+    {
+        return (vblock(i) % (S::VL / 16) * 16 + ((lane & 7) | (lane >> 1 & 8))) * S::DV;
+    }
 
-// Rows of no page are read as row 0 of the pool and take no part: a key by `ok`,
-// values by constants of 0.
-template <int D, int NT, bool KEY, bool ONE>
-__device__ __forceinline__ void read_ahead(const PagedAttnArgs &a, const Work &w, int i, Item &r)
-{
-    const int ng = ONE ? 1 : D / a.G;
-    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
-    r.ok = r.row >= 0;
-    const int64_t row = r.ok ? r.row : 0;
-    if constexpr (KEY) {
-        const int sl = item % (D / 32);
-        const int64_t g = row * ng + (ONE ? 0 : sl * 32 / a.G);
-        r.c = *reinterpret_cast<const uint4 *>(a.kp.c + row * (D / 2) + sl * 16);
-        r.s.x = a.kp.s[g];
-        r.z.x = a.kp.z[g];
-    } else {
-        const int dg = item % (D / 8);
-        const uint8_t *src = a.vp.c + row * (D / 2) + dg * 4;
-        r.c.x = *reinterpret_cast<const uint32_t *>(src);
-        r.c.y = *reinterpret_cast<const uint32_t *>(src + D / 2);
-        r.c.z = *reinterpret_cast<const uint32_t *>(src + D);
-        r.c.w = *reinterpret_cast<const uint32_t *>(src + 3 * (D / 2));
-        if constexpr (ONE) {  // four tokens' constants lie side by side
-            r.s = *reinterpret_cast<const uint2 *>(a.vp.s + row);
-            r.z = *reinterpret_cast<const uint2 *>(a.vp.z + row);
+    __device__ __forceinline__ int64_t group_row(int t) const
+    {
+        t = __builtin_amdgcn_readfirstlane(t);
+        const int64_t row = pool_row(a.map, a.hkv, w.b, t);
+        return row >= 0 ? row + (int64_t)h * a.map.page : -1;
+    }
+    __device__ __forceinline__ void look_keys(int t0)
+    {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i)
+            krow[i] = group_row(t0 + ((i * NT + wave * 64) / S::KL & ~15));
+    }
+    __device__ __forceinline__ void look_values(int t0)
+    {
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) {
+            vt[i] = t0 + vgroup(i) * 16;
+            vrow[i] = group_row(vt[i]);
+        }
+    }
+
+    // Groups of no page are read at row 0 of the pool (a pool has whole pages, of
+    // 16 rows at least) and take no part: a key by `kok`, values by constants of 0.
+    __device__ __forceinline__ void read_keys()
+    {
+        const int ng = ONE ? 1 : D / a.G;
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) {
+            kok[i] = krow[i] >= 0;
+            const int64_t row = kok[i] ? krow[i] : 0;
+            const uint32_t t = ktok(i) & 15, g = t * ng + (ONE ? 0 : ke(i, 0) / a.G);
+#pragma unroll
+            for (int wd = 0; wd < S::EK / 8; ++wd)
+                kc[i][wd] = *reinterpret_cast<const uint32_t *>(
+                    a.kp.c + row * (D / 2) + (t * (D / 2) + ke(i, wd) / 2));
+            ks[i] = (a.kp.s + row * ng)[g];
+            kz[i] = (a.kp.z + row * ng)[g];
+        }
+    }
+    __device__ __forceinline__ void read_values()
+    {
+        const int ng = ONE ? 1 : D / a.G;
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) {
+            const bool in = vrow[i] >= 0;
+            const int64_t row = in ? vrow[i] : 0;
+            const uint32_t t = 4 * vq();
+            const uint8_t *src = a.vp.c + row * (D / 2) + (t * (D / 2) + vd(i) / 2);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if constexpr (S::DV == 8)
+                    vc[i][x] = *reinterpret_cast<const uint32_t *>(src + x * (D / 2));
+                else if constexpr (S::DV == 4)
+                    vc[i][x] = *reinterpret_cast<const uint16_t *>(src + x * (D / 2));
+                else
+                    vc[i][x] = src[x * (D / 2)];
+            }
+            if constexpr (ONE) {  // four tokens' constants lie side by side
+                vs[i] = *reinterpret_cast<const uint2 *>(a.vp.s + row + t);
+                vz[i] = *reinterpret_cast<const uint2 *>(a.vp.z + row + t);
+            } else {
+                uint32_t s[4], z[4];
+                const uint32_t g = t * ng + vd(i) / a.G;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    s[x] = (a.vp.s + row * ng)[g + x * ng];
+                    z[x] = (a.vp.z + row * ng)[g + x * ng];
+                }
+                vs[i] = make_uint2(s[0] | (s[1] << 16), s[2] | (s[3] << 16));
+                vz[i] = make_uint2(z[0] | (z[1] << 16), z[2] | (z[3] << 16));
+            }
+            // tokens that no row sees take a weight of 0, and 0 times what a slot
+            // holds that was never written may be NaN
+            const int g0 = __builtin_amdgcn_readfirstlane(vt[i]);
+            if (__builtin_expect(!(in & (g0 + 16 <= w.hi) & (g0 >= w.low)), 0)) {
+                uint32_t keep[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int tt = g0 + (int)t + x;
+                    keep[x] = (in & (tt < w.hi) & ((tt >= w.low) | (tt < a.sinks))) ? 0xFFFFu : 0u;
+                }
+                const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
+                vs[i] = make_uint2(vs[i].x & k01, vs[i].y & k23);
+                vz[i] = make_uint2(vz[i].x & k01, vz[i].y & k23);
+            }
+        }
+    }
+
+    // Pair x of the keys (pairs in nib_order): a 16-byte unit is written with its
+    // fourth.
+    uint32_t unit[4];
+    __device__ __forceinline__ void put_keys(St &st, int x, const NibConst &nk)
+    {
+        const int i = x / (S::EK / 2), y = x % (S::EK / 2), wd = y / 4, j = y & 3;
+        const h2v s = bits_h2(perm_b32(ks[i], ks[i], 0x01000100u));
+        const h2v z = bits_h2(perm_b32(kz[i], kz[i], 0x01000100u));
+        const uint32_t c = j & 2 ? kc[i][wd] >> 8 : kc[i][wd];
+        const h2v v = fma2(j & 1 ? nib_pair<true>(c, nk) : nib_pair<false>(c, nk), s, z);
+        unit[j] = __builtin_bit_cast(uint32_t, v);
+        if (j == 3) {
+            *reinterpret_cast<uint4 *>(st.k + (ktok(i) * St::KP + ke(i, wd) * 2)) =
+                make_uint4(unit[0], unit[1], unit[2], unit[3]);
+            if (wd == 0)
+                st.ok[ktok(i) >> 4] = kok[i];  // (the lanes of a group write the same)
+        }
+    }
+    // Pair x of the values: dimension x / 2, tokens 0, 1 or 2, 3; a dimension's
+    // four tokens are written with its second.
+    uint32_t vpair;
+    __device__ __forceinline__ void put_values(St &st, int x, const NibConst &nk)
+    {
+        const int i = x / (S::DV * 2), y = x % (S::DV * 2), e = y >> 1;
+        const uint32_t bt = e >> 1;
+        // byte bt of two tokens in bytes 0 and 2
+        const uint32_t sel = bt | 0x0C00u | ((4 + bt) << 16) | 0x0C000000u;
+        const uint32_t c = y & 1 ? perm_b32(vc[i][3], vc[i][2], sel) : perm_b32(vc[i][1], vc[i][0], sel);
+        const h2v s = bits_h2(y & 1 ? vs[i].y : vs[i].x), z = bits_h2(y & 1 ? vz[i].y : vz[i].x);
+        const uint32_t v = __builtin_bit_cast(
+            uint32_t, fma2(e & 1 ? nib_pair<true>(c, nk) : nib_pair<false>(c, nk), s, z));
+        if (!(y & 1)) {
+            vpair = v;
         } else {
-            uint32_t s[4], z[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int64_t g = (row + x) * ng + dg * 8 / a.G;
-                s[x] = a.vp.s[g];
-                z[x] = a.vp.z[g];
-            }
-            r.s = make_uint2(s[0] | (s[1] << 16), s[2] | (s[3] << 16));
-            r.z = make_uint2(z[0] | (z[1] << 16), z[2] | (z[3] << 16));
-        }
-        // tokens that no row sees take a weight of 0, and 0 times what a slot
-        // holds that was never written may be NaN
-        if (!(r.ok & (r.t + 4 <= w.hi) & (r.t >= w.low))) {
-            uint32_t keep[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int t = r.t + x;
-                keep[x] = (r.ok & (t < w.hi) & ((t >= w.low) | (t < a.sinks))) ? 0xFFFFu : 0u;
-            }
-            const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
-            r.s = make_uint2(r.s.x & k01, r.s.y & k23);
-            r.z = make_uint2(r.z.x & k01, r.z.y & k23);
+            // quad q of a group: lane half q % 2, second 8 bytes for q / 2
+            const int q = vq(), d = vd(i) + e;
+            *reinterpret_cast<uint2 *>(st.v + (St::vrow(d) + St::vunit(d, 2 * vgroup(i) + (q & 1)) +
+                                               (q >> 1) * 8)) = make_uint2(vpair, v);
         }
     }
-}
-
-template <int D, int NT, bool KEY>
-__device__ __forceinline__ void put(Stage<D> &st, int i, const Item &r, const NibConst &nk)
-{
-    const int item = ((int)threadIdx.x + i * NT) & (2 * D - 1);
-    if constexpr (KEY) {
-        const int t = item / (D / 32), sl = item % (D / 32);
-        const h2v s = bits_h2(perm_b32(r.s.x, r.s.x, 0x01000100u));
-        const h2v z = bits_h2(perm_b32(r.z.x, r.z.x, 0x01000100u));
-        const uint32_t w[4] = {r.c.x, r.c.y, r.c.z, r.c.w};
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4 *>(st.k + t * (2 * D) + (((4 * sl + x) ^ (t & Stage<D>::KSW)) * 16)) =
-                unpack8(w[x], s, z, nk);
-        st.ok[t >> 4] = r.ok;  // (every lane of a 16-token group writes the same)
-    } else {
-        const int q = item / (D / 8), dg = item % (D / 8);
-        // tokens 4 q .. 4 q + 3: 16-token group q / 4, lane half q % 2, 8-byte
-        // piece (q / 2) % 2
-        const int unit = (q >> 2) * 2 + (q & 1), piece = (q >> 1) & 1;
-        const h2v s01 = bits_h2(r.s.x), s23 = bits_h2(r.s.y);
-        const h2v z01 = bits_h2(r.z.x), z23 = bits_h2(r.z.y);
-#pragma unroll
-        for (int bt = 0; bt < 4; ++bt) {
-            // byte bt of two tokens in bytes 0 and 2
-            const uint32_t sel = (uint32_t)bt | 0x0C00u | ((uint32_t)(4 + bt) << 16) | 0x0C000000u;
-            const uint32_t x01 = perm_b32(r.c.y, r.c.x, sel), x23 = perm_b32(r.c.w, r.c.z, sel);
-#pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-                const int d = dg * 8 + 2 * bt + hi;
-                const h2v a01 = hi ? nib_pair<true>(x01, nk) : nib_pair<false>(x01, nk);
-                const h2v a23 = hi ? nib_pair<true>(x23, nk) : nib_pair<false>(x23, nk);
-                *reinterpret_cast<uint2 *>(st.v + d * (2 * TT) + ((unit ^ ((d ^ (d >> 3)) & 7)) * 16) +
-                                           piece * 8) =
-                    make_uint2(__builtin_bit_cast(uint32_t, fma2(a01, s01, z01)),
-                               __builtin_bit_cast(uint32_t, fma2(a23, s23, z23)));
-            }
-        }
-    }
-}
+};
 
 // Block id -> (slot, split, cache head): heads next to each other, so that
 // with eight of them each XCD keeps to one head's cache; late slots (long
@@ -278,121 +379,77 @@ __device__ __forceinline__ Place place(const PagedAttnArgs &a, int slots)
     return p;
 }
 
-// Orders within a step, for the scheduler: what a wave issues runs in order, so
-// matrix products and vector instructions overlap only where they alternate.
-__device__ __forceinline__ void mix_softmax()
-{
-#if 0
-    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-#endif
-}
-
-__device__ __forceinline__ void mix_stage()
-{
-}
-
+// 32 query rows for each of NW waves.
 template <int D, int NW, bool ONE>
-__global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slots)
+__global__ __launch_bounds__(64 * NW)
+    __attribute__((amdgpu_waves_per_eu(NW == 8 ? 2 : 1, NW == 8 ? 2 : 1))) void k_paged_tile(PagedAttnArgs a, int slots)
 {
     constexpr int NT = 64 * NW, MR = 32 * NW;
     constexpr int KS = D / 16, DB = D / 32;
-    // stages: one that is multiplied, the next one, and one that is written while
-    // some wave may still be at the first (two, and a barrier more, where three
-    // do not fit)
-    constexpr int NB = D == 256 ? 2 : 3;
-    __shared__ __align__(16) Stage<D> st[NB];
-    __shared__ int shb;
+    // A stage holds 64 tokens (32 for D = 256).  While one's scores are taken and
+    // the last one's values are added, the next but one is written.
+    constexpr int TS = D == 256 ? 32 : 64, NB = D == 256 ? 4 : 3;
+    using St = Stage<D, TS>;
+    using Sh = Share<D, TS, NT>;
+    __shared__ __align__(16) St st[NB];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, hf = lane >> 5;
     const Place pl = place(a, slots);
-    const Work w = find_work<MR>(a, pl.slot, &shb);
+    const Work w = find_work<MR>(a, pl.slot);
     if (w.rows == 0 || pl.split >= w.used)
         return;
     const float inf = __builtin_inff();
     const float c2 = a.sm_scale * 1.44269504088896340736f;  // log2(e)
 
-    // this lane's query: row, batch row, head, position
-    const int row = min(w.row0 + wave * 32 + n, w.rows - 1);
-    const bool live = w.row0 + wave * 32 + n < w.rows;
-    const int qi = row / a.rep;
-    const int head = pl.h * a.rep + (row - qi * a.rep);
-    const int p = w.pos0 + qi;
+    // this lane's query (past the last row, the last one again)
+    const int row = w.row0 + wave * 32 + n, qrow = min(row, w.rows - 1), qi = qrow / a.rep;
+    const int p = w.pos0 + qi, head = pl.h * a.rep + (qrow - qi * a.rep);
     const int64_t trow = w.tok0 + qi;
-    const int wfirst = a.window > 0 ? p - a.window : -1;  // tokens up to here only as sinks
-    v8h qb[KS];
-    {
-        const uint16_t *qr = a.q + trow * a.q_stride + (int64_t)head * D;
+    const uint16_t *qr = a.q + trow * a.q_stride + (int64_t)head * D;
+    uint4 qraw[KS];
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
-            qb[k] = __builtin_bit_cast(
-                v8h, nib_order(*reinterpret_cast<const uint4 *>(qr + 16 * k + 8 * hf)));
-    }
+    for (int k = 0; k < KS; ++k)
+        qraw[k] = *reinterpret_cast<const uint4 *>(qr + 16 * k + 8 * hf);
 
     v16f o[DB];
+    float m = -inf, l = 0.0f;  // reference (log2 units); this lane's half of the sum
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             o[d][r] = 0.0f;
-    float m = -inf, l = 0.0f;  // in log2 units; this lane's half of the sum
 
     const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
-    auto token0 = [&](int i) { return paged::step_token(w, i < end ? i : end - 1); };
     const int pmin = w.pos0 + w.row0 / a.rep, pmax = w.pos0 + (min(w.row0 + MR, w.rows) - 1) / a.rep;
 
-    // scores of the 32 tokens of half u: register r holds token
-    // 32 u + 8 (r / 4) + 4 hf + r % 4
-    auto score = [&](const Stage<D> &sg, int u) {
-        v16f s;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[r] = 0.0f;
-        const int t = 32 * u + n;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            const v8h kf = *reinterpret_cast<const v8h *>(
-                sg.k + t * (2 * D) + (((2 * k + hf) ^ (t & Stage<D>::KSW)) * 16));
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qb[k], s, 0, 0, 0);
-        }
-        return s;
+    auto weight = [&](const v16f &s, v8h *pb, float ms, int r) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -ms));
+        pb[r >> 3][r & 7] = (_Float16)e;
+        return e;
     };
-    // their weights as the value product's B operands, and the sums
-    auto weigh = [&](const v16f &s, v8h *pb, float ms) {
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // scores of tokens t0 .. t0 + 31 (register r holds t0 + 8 (r / 4) + 4 hf +
+    // r % 4) that a query does not see
+    auto hide = [&](v16f &s, int t0, const int *ok) {
+        const int first = a.window > 0 ? p - a.window : -1;  // up to here only as sinks
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c2, -ms));
-            sum[r & 3] += e;
-            pb[r >> 3][r & 7] = (_Float16)e;
-        }
-        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    };
-    auto hide = [&](v16f &s, int t0, const int *ok, int u) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int t = t0 + 32 * u + 8 * (r >> 2) + 4 * hf + (r & 3);
-            const bool see = (t <= p) & ((t > wfirst) | (t < a.sinks)) & (ok[2 * u + (r >> 3)] != 0);
+            const int t = t0 + 8 * (r >> 2) + 4 * hf + (r & 3);
+            const bool see = (t <= p) & ((t > first) | (t < a.sinks)) & (ok[r >> 3] != 0);
             s[r] = see ? s[r] : -inf;
         }
     };
-    // takes the weights' sum; where they pass what fp16 holds, or there is no
-    // reference yet, the reference moves to the largest score
-    auto settle = [&](const v16f &s, v8h *pb, float ls) {
-        if (__builtin_expect(__any(!(ls <= 0x1p15f) | (m == -inf)), 0)) {
+    // Takes the weights' sums; where they pass what fp16 holds, or there is no
+    // reference yet, the reference moves to the largest score.
+    auto settle = [&](const v16f &s, v8h *pb, float sum) {
+        if (__builtin_expect(__any(!(sum <= 0x1p15f) | (m == -inf)), 0)) {
             float mt = s[0];
 #pragma unroll
             for (int r = 1; r < 16; ++r)
                 mt = fmaxf(mt, s[r]);
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt),
-                                                             false, false);
-            const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2);
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt),
+                                                             __float_as_uint(mt), false, false);
+            const float mn =
+                fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2);
             const float ms = mn > -inf ? mn : 0.0f;  // nothing seen so far: weights 0
             const float f = m > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.0f;
             m = mn;
@@ -400,126 +457,215 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                for (int r = 0; r < 16; ++r)
                     o[d][r] *= f;
-                    asm volatile("" : "+v"(o[d]));
-                }
-            ls = weigh(s, pb, ms);
+            sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                sum += weight(s, pb, ms, r);
         }
-        l += ls;
+        l += sum;
     };
-    auto add_values = [&](const Stage<D> &sg, int u, const v8h *pb) {
+    // One round of 32 tokens: the softmax of the scores sc, while the matrix cores
+    // take the next round's scores sn (half uk of stage sk) and add the last
+    // round's values (half uv of stage sv, weights pp).  A wave issues in order,
+    // so the two overlap only where they alternate: each of 2 KS parts has its
+    // share of the products, of the softmax, of the reads of a part ahead, and of
+    // the staging (also(c)), and the scheduler is kept from gathering them.
+    auto round = [&](const v16f &sc, v16f &sn, const v8h *pp, v8h *pb, const St &sk, int uk,
+                     const St &sv, int uv, const v8h *qb, auto also) {
+        const uint8_t *kb = sk.k + (n * St::KP + hf * 16), *vr = sv.v + St::vrow(n);
+        const uint8_t *vb[2] = {vr + St::vunit(n, 4 * uv + hf), vr + St::vunit(n, 4 * uv + 2 + hf)};
+        auto kfrag = [&](int k) {
+            return *reinterpret_cast<const v8h *>(kb + (32 * uk * St::KP + 32 * k));
+        };
+        auto vfrag = [&](int c) {
+            const int db = c % DB;
+            return *reinterpret_cast<const v8h *>(vb[(c / DB) ^ (db & 1)] + 32 * db * St::VP);
+        };
+        constexpr int AHEAD = 2;
+        v8h kf[KS], vf[2 * DB];  // KS == 2 DB
+        float ls[2] = {0.0f, 0.0f};
+        const float ms = m > -inf ? m : 0.0f;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int unit = (2 * u + x) * 2 + hf;
+        for (int r = 0; r < 16; ++r)
+            sn[r] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const int dim = 32 * d + n;
-                const v8h vf = *reinterpret_cast<const v8h *>(
-                    sg.v + dim * (2 * TT) + ((unit ^ ((dim ^ (dim >> 3)) & 7)) * 16));
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pb[x], o[d], 0, 0, 0);
-            }
+        for (int c = 0; c < AHEAD; ++c) {
+            kf[c] = kfrag(c);
+            vf[c] = vfrag(c);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < KS; ++c) {
+            sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c], qb[c], sn, 0, 0, 0);
+            if (c + AHEAD < KS)
+                kf[c + AHEAD] = kfrag(c + AHEAD);
+#pragma unroll
+            for (int r = 16 * c / KS; r < 16 * (c + 1) / KS; r += 2) {
+                if (KS == 16 && (c & 1))
+                    continue;  // a part's share is one weight: two with every other
+                ls[0] += weight(sc, pb, ms, r);
+                ls[1] += weight(sc, pb, ms, r + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            o[c % DB] =
+                __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[c], pp[c / DB], o[c % DB], 0, 0, 0);
+            if (c + AHEAD < KS)
+                vf[c + AHEAD] = vfrag(c + AHEAD);
+            also(c);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        settle(sc, pb, ls[0] + ls[1]);
     };
 
     if (begin < end) {
-        using Sh = Share<D, NT>;
+        constexpr int H = 64 / TS;      // stages of a step
+        constexpr int PM = Sh::PAIRS / KS;  // pairs with a part
         const NibConst nk = nib_const();
-        // 0: this wave stages keys, 1: values, 2: nothing
-        const int role = Sh::PART ? __builtin_amdgcn_readfirstlane(tid / (2 * D)) : 0;
-        Item kv[Sh::PART ? 1 : 2][Sh::N];
-        // f(a kind of item, its items) for what this wave stages, then once `also`
-        auto each = [&](auto f, auto also) {
-            if constexpr (Sh::PART) {
-                if (role == 0) {
-                    f(std::true_type(), kv[0]);
-                    also();
-                } else if (NT <= 4 * D || role == 1) {
-                    f(std::false_type(), kv[0]);
-                    also();
-                } else {
-                    also();
-                }
-            } else {
-                f(std::true_type(), kv[0]);
-                f(std::false_type(), kv[1]);
-                also();
+        // first token of stage j; past the last one, the last one again
+        auto token0 = [&](int j) {
+            const int k = min(j, (end - begin) * H - 1);
+            return paged::step_token(w, begin + k / H) + k % H * TS;
+        };
+        Ahead<D, TS, NT, ONE> ah{a, w, pl.h, __builtin_amdgcn_readfirstlane(wave), lane};
+        auto put_all = [&](auto &from, St &to) {
+#pragma unroll
+            for (int x = 0; x < Sh::PAIRS; ++x) {
+                from.put_keys(to, x, nk);
+                from.put_values(to, x, nk);
             }
         };
-        auto look = [&](int step) {
-            return [&, step](auto key, Item *r) {
-#pragma unroll
-                for (int i = 0; i < Sh::N; ++i)
-                    look_up<D, NT, decltype(key)::value>(a, w, pl.h, token0(step), i, r[i]);
-            };
+        auto next = [&](int j) {  // reads what was looked up, looks stage j up
+            ah.read_keys();
+            ah.look_keys(token0(j));
+            ah.read_values();
+            ah.look_values(token0(j));
         };
-        auto read = [&](auto key, Item *r) {
+        // two stages' pages are looked up, then read, at once
+        auto first = ah;
+        first.look_keys(token0(0));
+        first.look_values(token0(0));
+        ah.look_keys(token0(1));
+        ah.look_values(token0(1));
+        first.read_keys();
+        first.read_values();
+        next(2);
+        put_all(first, st[0]);
+        if constexpr (TS == 32) {
+            put_all(ah, st[1]);
+            next(3);
+        } else {  // the values follow in the first round
 #pragma unroll
-            for (int i = 0; i < Sh::N; ++i)
-                read_ahead<D, NT, decltype(key)::value, ONE>(a, w, i, r[i]);
-        };
-        auto write = [&](Stage<D> &to) {
-            return [&](auto key, Item *r) {
+            for (int x = 0; x < Sh::PAIRS; ++x)
+                ah.put_keys(st[1], x, nk);
+            ah.read_keys();
+            ah.look_keys(token0(3));
+        }
+        v8h qb[KS];
 #pragma unroll
-                for (int i = 0; i < Sh::N; ++i)
-                    put<D, NT, decltype(key)::value>(to, i, r[i], nk);
-            };
-        };
-        auto nothing = [] {};
-        each(look(begin), nothing);
-        each(read, nothing);
-        each(write(st[0]), nothing);
-        each(look(begin + 1), nothing);
-        each(read, nothing);
-        each(look(begin + 2), nothing);
+        for (int k = 0; k < KS; ++k)
+            qb[k] = __builtin_bit_cast(v8h, nib_order(qraw[k]));
         __syncthreads();
-        v16f s0 = score(st[0], 0), s1;
-        int cur = 0;
-        for (int i = begin; i < end; ++i) {
-            const int t0 = token0(i);
-            const Stage<D> &sc = st[cur];
-            const int nx = cur + 1 < NB ? cur + 1 : 0;
-            const int ok[4] = {sc.ok[0], sc.ok[1], sc.ok[2], sc.ok[3]};
-            const bool edge = !(ok[0] & ok[1] & ok[2] & ok[3]) || t0 + TT - 1 > pmin ||
-                              (a.window > 0 && t0 <= pmax - a.window);
-            v8h pb[2];
-            if (edge)
-                hide(s0, t0, ok, 0);
-            s1 = score(sc, 1);
-            float ls = weigh(s0, pb, m > -inf ? m : 0.0f);
-            mix_softmax();
-            settle(s0, pb, ls);
-            each(
-                [&](auto key, Item *r) {
-                    write(st[nx])(key, r);
-                    read(key, r);
-                    look(i + 3)(key, r);
-                },
-                nothing);
-            add_values(sc, 0, pb);
-            if (edge)
-                hide(s1, t0, ok, 1);
-            __syncthreads();  // the next step's stage is whole
-            s0 = score(st[nx], 0);
-            ls = weigh(s1, pb, m > -inf ? m : 0.0f);
-            mix_softmax();
-            settle(s1, pb, ls);
-            add_values(sc, 1, pb);
-            if constexpr (NB == 2)
-                __syncthreads();  // this one may be overwritten
-            cur = nx;
+
+        v16f sa, sb;  // scores of this round and the next, in turn
+        v8h pa[2], pb[2];  // weights likewise
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                pb[x][e] = (_Float16)0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            sa[r] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            sa = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                *reinterpret_cast<const v8h *>(st[0].k + n * St::KP + hf * 16 + 32 * k), qb[k], sa,
+                0, 0, 0);
+        const int stages = (end - begin) * H;
+        if constexpr (TS == 64) {
+            int last = 0, cur = 0;
+            for (int j = 0; j < stages; ++j) {
+                const int t0 = token0(j);
+                const int nx = cur + 1 < NB ? cur + 1 : 0, n2 = nx + 1 < NB ? nx + 1 : 0;
+                const int ok[4] = {st[cur].ok[0], st[cur].ok[1], st[cur].ok[2], st[cur].ok[3]};
+                const bool edge = !(ok[0] & ok[1] & ok[2] & ok[3]) || t0 + TS - 1 > pmin ||
+                                  (a.window > 0 && t0 <= pmax - a.window);
+                if (edge)
+                    hide(sa, t0, ok);
+                round(sa, sb, pb, pa, st[cur], 1, st[last], 1, qb, [&](int c) {
+#pragma unroll
+                    for (int x = 0; x < PM; ++x)
+                        ah.put_values(st[nx], c * PM + x, nk);
+                });
+                ah.read_values();
+                ah.look_values(token0(j + 3));
+                if (edge)
+                    hide(sb, t0 + 32, ok + 2);
+                __syncthreads();  // stage nx is whole, every wave is through with the last
+                round(sb, sa, pa, pb, st[nx], 0, st[cur], 0, qb, [&](int c) {
+#pragma unroll
+                    for (int x = 0; x < PM; ++x)
+                        ah.put_keys(st[n2], c * PM + x, nk);
+                });
+                ah.read_keys();
+                ah.look_keys(token0(j + 4));
+                last = cur;
+                cur = nx;
+            }
+#pragma unroll
+            for (int c = 0; c < KS; ++c)
+                o[c % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    *reinterpret_cast<const v8h *>(
+                        st[last].v + St::vrow(32 * (c % DB) + n) +
+                        St::vunit(32 * (c % DB) + n, 4 + c / DB * 2 + hf)),
+                    pb[c / DB], o[c % DB], 0, 0, 0);
+        } else {
+            int last = 0, cur = 0;
+            for (int j = 0; j < stages; j += 2)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int t0 = token0(j + h);
+                    const int nx = (cur + 1) & 3, n2 = (cur + 2) & 3;
+                    const int ok[2] = {st[cur].ok[0], st[cur].ok[1]};
+                    const bool edge = !(ok[0] & ok[1]) || t0 + TS - 1 > pmin ||
+                                      (a.window > 0 && t0 <= pmax - a.window);
+                    if (edge)
+                        hide(h ? sb : sa, t0, ok);
+                    auto put = [&](int c) {
+#pragma unroll
+                        for (int x = 0; x < PM; ++x) {
+                            ah.put_keys(st[n2], c * PM + x, nk);
+                            ah.put_values(st[n2], c * PM + x, nk);
+                        }
+                    };
+                    if (h)
+                        round(sb, sa, pa, pb, st[nx], 0, st[last], 0, qb, put);
+                    else
+                        round(sa, sb, pb, pa, st[nx], 0, st[last], 0, qb, put);
+                    next(j + h + 4);
+                    __syncthreads();
+                    last = cur;
+                    cur = nx;
+                }
+#pragma unroll
+            for (int c = 0; c < KS; ++c)
+                o[c % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    *reinterpret_cast<const v8h *>(
+                        st[last].v + St::vrow(32 * (c % DB) + n) +
+                        St::vunit(32 * (c % DB) + n, c / DB * 2 + hf)),
+                    pb[c / DB], o[c % DB], 0, 0, 0);
         }
     }
 
-    {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false,
-                                                         false);
-        l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    }
-    if (!live)
+    const auto sw =
+        __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    const float lt = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (row >= w.rows)
         return;
     if (w.used == 1) {
-        const float f = l > 0.0f ? 1.0f / l : 0.0f;
+        const float f = lt > 0.0f ? 1.0f / lt : 0.0f;
         uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -531,7 +677,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
                 *reinterpret_cast<uint2 *>(dst + 32 * d + 2 * r + 4 * hf) = v;
             }
     } else {
-        const int64_t pr = (trow * a.hq + head) * a.splits + pl.split;
+        const int64_t pr = part_of(a, w, row, pl.h) + pl.split;
         float *dst = a.part_o + pr * D;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -540,7 +686,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_tile(PagedAttnArgs a, int slo
                 *reinterpret_cast<float4 *>(dst + 32 * d + 2 * r + 4 * hf) =
                     make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
         if (hf == 0)
-            *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(m, l);
+            *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(m, lt);
     }
 }
 
@@ -605,11 +751,10 @@ __global__ __launch_bounds__(64 * ROWS_W)
     constexpr int VD = D / 16;  // dimensions of a lane in the value product
     constexpr int RED = ROWS_W * MR * (D + 2) * 4, RING = ROWS_W * ROWS_NS * Ring::STAGE;
     __shared__ __align__(16) uint8_t lds[RED > RING ? RED : RING];
-    __shared__ int shb;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 15, g = lane >> 4;
     const Place pl = place(a, slots);
-    const Work w = find_work<MR>(a, pl.slot, &shb);
+    const Work w = find_work<MR>(a, pl.slot);
     if (w.rows == 0 || pl.split >= w.used)
         return;
     const float inf = __builtin_inff();
@@ -934,7 +1079,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
             *reinterpret_cast<uint32_t *>(a.out + trow * a.out_stride + (int64_t)head * D + d) =
                 (uint32_t)f2h(oa * f) | ((uint32_t)f2h(ob * f) << 16);
         } else {
-            const int64_t pr = (trow * a.hq + head) * a.splits + pl.split;
+            const int64_t pr = part_of(a, w, rr, pl.h) + pl.split;
             *reinterpret_cast<float2 *>(a.part_o + pr * D + d) = make_float2(oa, ob);
             if (d == 0)
                 *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(mx, lt);
@@ -950,11 +1095,10 @@ __global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a)
 {
     constexpr int E = D / 64;  // elements of a lane
     constexpr int RPB = 4 / WPR;
-    __shared__ int shb;
     __shared__ float red[WPR > 1 ? 4 : 1][D + 2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int h = (int)(blockIdx.x % (uint32_t)a.hkv);
-    const Work w = find_work<MR>(a, (int)(blockIdx.x / (uint32_t)a.hkv), &shb);
+    const Work w = find_work<MR>(a, (int)(blockIdx.x / (uint32_t)a.hkv));
     if (w.rows == 0 || w.used == 1)
         return;
     const float inf = __builtin_inff();
@@ -963,7 +1107,7 @@ __global__ __launch_bounds__(256) void k_paged_combine(PagedAttnArgs a)
         const bool live = r < MR && w.row0 + r < w.rows;
         const int head = h * a.rep + (row - qi * a.rep);
         const int64_t trow = w.tok0 + qi;
-        const int64_t pr = (trow * a.hq + head) * a.splits;
+        const int64_t pr = part_of(a, w, row, h);
         float mx = -inf;
         for (int s = lane; s < w.used; s += 64)
             mx = fmaxf(mx, a.part_ml[2 * (pr + s)]);
@@ -1025,23 +1169,21 @@ template <int D, int NW>
 hipError_t go_tile(const PagedAttnArgs &a, hipStream_t s)
 {
     constexpr int MR = 32 * NW;
-    const int slots = (int)paged::slots(a.map.T, a.map.B, a.rep, MR);
+    const int slots = (int)paged::slots({a.which, MR}, a.map.T, a.map.B, a.rep);
     const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
     if (a.G == D)
         hipLaunchKernelGGL((k_paged_tile<D, NW, true>), grid, dim3(64 * NW), 0, s, a, slots);
     else
         hipLaunchKernelGGL((k_paged_tile<D, NW, false>), grid, dim3(64 * NW), 0, s, a, slots);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1)
-        return e;
-    return go_combine<D, MR>(a, slots, s);
+    return e != hipSuccess || a.splits == 1 ? e : go_combine<D, MR>(a, slots, s);
 }
 
 template <int D>
 hipError_t go_few(const PagedAttnArgs &a, hipStream_t s)
 {
     constexpr int MR = paged::FEW_ROWS;
-    const int slots = (int)paged::slots(a.map.T, a.map.B, a.rep, MR);
+    const int slots = (int)paged::slots({a.which, MR}, a.map.T, a.map.B, a.rep);
     const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
     hipLaunchKernelGGL((k_paged_rows<D>), grid, dim3(64 * ROWS_W), 0, s, a, slots);
     hipError_t e = hipGetLastError();
@@ -1064,12 +1206,12 @@ hipError_t go_rows(const PagedAttnArgs &a, int rows, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_paged_attention(const PagedAttnArgs &a, const paged::Plan &p, hipStream_t s)
+hipError_t launch_paged_attention(const PagedAttnArgs &a, int rows, hipStream_t s)
 {
     switch (a.D) {
-    case 64: return go_rows<64>(a, p.rows, s);
-    case 128: return go_rows<128>(a, p.rows, s);
-    case 256: return go_rows<256>(a, p.rows, s);
+    case 64: return go_rows<64>(a, rows, s);
+    case 128: return go_rows<128>(a, rows, s);
+    case 256: return go_rows<256>(a, rows, s);
     }
     return hipErrorInvalidValue;
 }

@@ -98,11 +98,56 @@ QUAROT_HD int step_token(const Span &w, int i)
     return (i < w.lo ? i : i - w.lo + w.first) * STEP;
 }
 
-struct Plan {
+// Which sequences a launch works on, by their query rows.  FEW takes a block row
+// for each sequence, the others one for each slot.
+enum Which { ALL, MANY /* more than FEW_ROWS */, FEW /* at most FEW_ROWS */ };
+
+struct Part {
+    Which which;
     int rows;    // query rows of a block
     int splits;  // blocks that share a block row's tokens, at most
     int least;   // steps of a split, at least
 };
+
+struct Plan {
+    int n;  // launches
+    Part part[2];
+};
+
+// Block rows of a launch.
+inline int64_t slots(const Part &p, int64_t T, int64_t B, int64_t rep)
+{
+    return p.which == FEW ? B : T * rep / p.rows + B;
+}
+
+// Rows that a launch keeps partial results of: those of a sequence from
+// part_row(...) on.
+inline int64_t part_rows(const Part &p, int64_t T, int64_t B, int64_t rep)
+{
+    return p.splits == 1 ? 0 : p.which == FEW ? B * FEW_ROWS : T * rep;
+}
+
+QUAROT_HD int64_t part_row(Which which, int64_t b, int64_t tok0, int64_t rep)
+{
+    return which == FEW ? b * FEW_ROWS : tok0 * rep;
+}
+
+inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
+{
+    const int least = (int)std::min<int64_t>(16, std::max<int64_t>(8, steps * B * hkv / 2048));
+    const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, (1 << 20) / (B * hkv)});
+    return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
+}
+
+inline Part tile_part(Which which, int64_t steps, int64_t rows, int64_t T, int64_t B, int64_t hkv,
+                      int64_t rep, int64_t D)
+{
+    Part p{which, D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256, 1, 4};
+    const int64_t blocks = hkv * std::max<int64_t>((T * rep + p.rows - 1) / p.rows, which == MANY ? 1 : B);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, 512 / blocks, 128,
+                                                            2048 / (hkv * slots(p, T, B, rep))}));
+    return p;
+}
 
 // T new tokens of B sequences, hkv cache heads with rep query heads each, at
 // most max_len cached tokens.  Only a rule of speed: any content of cu and len
@@ -110,28 +155,17 @@ struct Plan {
 inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int64_t G,
                  int64_t max_len, int64_t window, int64_t sinks)
 {
-    Plan p;
-    // query rows of a sequence, on average
-    const int64_t rows = (T * rep + B - 1) / B;
+    // query rows of a sequence: on average, and of the longest at most (where
+    // the others have a token each)
+    const int64_t rows = (T * rep + B - 1) / B, most = std::max<int64_t>(T - B + 1, 1) * rep;
     const int64_t seen = window > 0 ? std::min(max_len, window + sinks + T / B) : max_len;
     const int64_t steps = (seen + STEP - 1) / STEP;
-    if (rows <= FEW_ROWS && G == D) {
-        p.rows = FEW_ROWS;
-        p.least = (int)std::min<int64_t>(16, std::max<int64_t>(8, steps * B * hkv / 2048));
-        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((steps + p.least - 1) / p.least, 128));
-        return p;
-    }
-    p.rows = D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-    const int64_t blocks = B * ((rows + p.rows - 1) / p.rows) * hkv;
-    p.least = 4;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, 512 / blocks, 128}));
-    return p;
-}
-
-// Blocks of a launch along the sequences.
-inline int64_t slots(int64_t T, int64_t B, int64_t rep, int mr)
-{
-    return T * rep / mr + B;
+    if (G != D || rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
+        return Plan{1, {tile_part(ALL, steps, rows, T, B, hkv, rep, D)}};
+    if (rows <= FEW_ROWS && most <= 4 * FEW_ROWS)
+        return Plan{1, {few_part(ALL, steps, B, hkv)}};
+    return Plan{2, {tile_part(MANY, steps, std::max(rows, most / 4), T, B, hkv, rep, D),
+                    few_part(FEW, steps, B, hkv)}};
 }
 
 }  // namespace paged

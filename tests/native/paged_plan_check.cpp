@@ -65,7 +65,7 @@ static void batches(std::mt19937 &rng)
         }
         const int T = cu[B] + rng() % 3, cap = rng() % 5 ? 2048 : 320;
         std::vector<int> seen((size_t)T * rep, 0);
-        const int64_t total = slots(T, B, rep, mr);
+        const int64_t total = slots(Part{ALL, mr, 1, 1}, T, B, rep);
         for (int64_t slot = 0; slot < total; ++slot)
             for (int b = 0; b < B; ++b) {
                 const int64_t f = first_slot((int64_t)cu[b] * rep, b, mr);
@@ -128,7 +128,7 @@ static void bad_contents(std::mt19937 &rng)
 
 static void plans()
 {
-    bool taken[4] = {}, cut = false;
+    bool taken[4] = {}, cut = false, two = false;
     for (int64_t T : {1, 2, 16, 64, 333, 2048, 16384, 1 << 20})
         for (int64_t B : {1, 2, 16, 64, 300, 5000})
             for (int64_t hkv : {1, 2, 8, 64})
@@ -138,13 +138,27 @@ static void plans()
                             for (int64_t window : {0, 1, 1000, 1 << 30}) {
                                 const Plan p = plan(T, B, hkv, rep, D, T % 3 ? D : 32, len, window,
                                                     1 << 30);
-                                CHECK(p.least >= 1 && (int64_t)p.least * p.splits < 1 << 20, "least");
-                                CHECK(p.splits >= 1 && p.splits <= 128, "splits %d", p.splits);
-                                CHECK(p.rows == 16 || p.rows == 64 || p.rows == 128 || p.rows == 256, "rows");
-                                taken[p.rows == 16 ? 0 : p.rows == 64 ? 1 : p.rows == 128 ? 2 : 3] = true;
-                                cut = cut || p.splits > 1;
+                                CHECK(p.n == 1 || p.n == 2, "launches");
+                                // every sequence in one launch
+                                CHECK(p.n == 1 ? p.part[0].which == ALL
+                                               : p.part[0].which == MANY && p.part[1].which == FEW,
+                                      "which");
+                                for (int i = 0; i < p.n; ++i) {
+                                    const Part &t = p.part[i];
+                                    CHECK(t.least >= 1 && (int64_t)t.least * t.splits < 1 << 20, "least");
+                                    CHECK(t.splits >= 1 && t.splits <= 128, "splits %d", t.splits);
+                                    CHECK(t.rows == 16 || t.rows == 64 || t.rows == 128 || t.rows == 256, "rows");
+                                    CHECK(t.rows != 16 || T % 3 || D == 32, "whole groups");
+                                    CHECK(t.which != FEW || t.rows == FEW_ROWS, "few");
+                                    // partial rows of every block fit
+                                    CHECK(t.splits == 1 || part_row(t.which, B - 1, T - 1, rep) <
+                                                               part_rows(t, T, B, rep), "partial rows");
+                                    taken[t.rows == 16 ? 0 : t.rows == 64 ? 1 : t.rows == 128 ? 2 : 3] = true;
+                                    cut = cut || t.splits > 1;
+                                }
+                                two = two || p.n == 2;
                             }
-    CHECK(taken[0] && taken[1] && taken[2] && taken[3] && cut, "a kernel is never taken");
+    CHECK(taken[0] && taken[1] && taken[2] && taken[3] && cut && two, "a kernel is never taken");
 }
 
 int main()

@@ -271,6 +271,20 @@ def test_long_sequences_are_split(dev, orc, new, total, H, hkv, D, G):
     check(dev, orc, bt, H, max_seq_len=1)
 
 
+@pytest.mark.parametrize("D,G,H,hkv,page", [(64, 64, 8, 8, 16), (128, 128, 16, 2, 64),
+                                            (128, 128, 5, 5, 48), (256, 256, 16, 1, 32)])
+@pytest.mark.parametrize("new", [[1, 40, 2, 16, 17, 0, 3], [64, 1, 1], [1, 1, 1, 1, 300],
+                                 [1] * 70 + [90] + [2] * 70, [0, 0, 33, 0, 0], [1] * 130 + [500]])
+def test_mixed_batches(dev, orc, D, G, H, hkv, page, new):
+    """Long and short sequences of a batch go through kernels of their own."""
+    total = [n + (37 * i) % 90 + (3 * (len(new) < 10) << (i % 9)) for i, n in enumerate(new)]
+    bt = Batch(11, new, total, hkv, D, G, page)
+    check(dev, orc, bt, H)
+    check(dev, orc, bt, H, window=50, sinks=5)
+    if len(new) < 10:  # both of their sums over splits
+        check(dev, orc, bt, H, max_seq_len=30000)
+
+
 def test_large_scores(dev, orc):
     """Queries whose scores reach hundreds: one token takes all the weight."""
     check(dev, orc, Batch(9, [1, 40], [300, 300], 2, 128, 128, 16), 8, sigma=60.0)
