@@ -59,7 +59,7 @@ struct Span {
 
 // Sequence of rows cu0 .. cu1 - 1 of a batch of T, len cached tokens; block
 // `slot - first_slot` of it; a table of cap positions; window 0: none; at most
-// `splits` splits of `least` steps each, or more where they would not do.  Any content of cu0, cu1 and len gives a span inside the
+// `splits` equal splits, for each `least` steps one.  Any content of cu0, cu1 and len gives a span inside the
 // batch and the table.  cap and T are at most 2^30, window and sinks too.
 QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t block, int mr,
                     int window, int sinks, int splits, int least)
@@ -85,8 +85,10 @@ QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t 
         w.lo = w.lo < w.first ? w.lo : w.first;
         w.steps += w.lo - w.first;
     }
-    w.per = (w.steps + splits - 1) / splits;
-    w.per = w.per > least ? w.per : least;
+    w.used = (w.steps + least - 1) / least;
+    w.used = w.used < 1 ? 1 : w.used > splits ? splits : w.used;
+    w.per = (w.steps + w.used - 1) / w.used;
+    w.per = w.per > 1 ? w.per : 1;
     w.used = (w.steps + w.per - 1) / w.per;
     w.used = w.used > 1 ? w.used : 1;
     return w;
