@@ -134,9 +134,16 @@ QUAROT_HD int64_t part_row(Which which, int64_t b, int64_t tok0, int64_t rep)
     return which == FEW ? b * FEW_ROWS : tok0 * rep;
 }
 
+// Few rows: splits of such a length that 512 of them, two a CU, hold the steps of a
+// batch of full sequences.  Shorter ones pay for their starts and their joining (64
+// sequences of 1024 tokens and 8 heads: 27 us in splits of 8 steps, 21 whole; 256
+// of 1 .. 2048 tokens: 97 and 75), longer ones leave CUs idle behind the longest
+// (64 of 1 .. 8192: 73 us in splits of 32 steps, 89 of 64), and few steps do best
+// in pieces of 4 (one of 4096: 10.5 us, 13 of 8, 21 of 24; but one of 32768: 22 of
+// 4, 19 of 8).
 inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
 {
-    const int least = (int)std::min<int64_t>(16, std::max<int64_t>(8, steps * B * hkv / 2048));
+    const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * B * hkv / 512));
     const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, (1 << 20) / (B * hkv)});
     return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
 }
