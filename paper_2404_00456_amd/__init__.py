@@ -903,10 +903,13 @@ def _half_rows(t: torch.Tensor, name: str):
 
 def _token_rows(t: torch.Tensor, name: str):
     """(address, elements between tokens) of fp16 [T, heads, D]."""
-    _half_rows(t, name)
+    if t.dtype != torch.float16 or t.dim() != 3:
+        _half_rows(t, name)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     T, H, D = t.shape
+    if t.is_contiguous():
+        return t.data_ptr(), H * D
     st = t.stride()
     if (D > 1 and st[2] != 1) or (H > 1 and st[1] != D):
         raise ValueError(f"{name}: the heads of a token must follow one another, got strides {st}")
@@ -916,7 +919,7 @@ def _token_rows(t: torch.Tensor, name: str):
 def _on_device(dev, **tensors):
     """Every tensor on `dev`, and `dev` the current device (whose stream the
     call runs on)."""
-    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+    if dev.type == "cuda" and dev.index != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on {dev}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
     for name, t in tensors.items():
@@ -925,9 +928,9 @@ def _on_device(dev, **tensors):
 
 
 def _sections(sections, half: int):
-    """The axis of each of `half` pairs as a host array, and the axes: runs of
-    the given lengths for axis 0, 1, .. (a list of ints), or the axis of each
-    pair itself (a sequence of `half` axes given as bytes)."""
+    """The axis of each of `half` pairs as bytes (None: one axis), and the axes:
+    runs of the given lengths for axis 0, 1, .. (a list of ints), or the axis of
+    each pair itself (a sequence of `half` axes given as bytes)."""
     if sections is None:
         return None, 1
     if isinstance(sections, (bytes, bytearray)):
@@ -935,44 +938,46 @@ def _sections(sections, half: int):
         n = max(axes, default=0) + 1
     else:
         sections = [int(x) for x in sections]
-        if any(x < 0 for x in sections) or not 1 <= len(sections) <= 4:
-            raise ValueError(f"sections must be the pairs of 1 to 4 axes, got {sections}")
-        axes = b"".join(bytes([a]) * x for a, x in enumerate(sections))
         n = len(sections)
+        if any(x < 0 for x in sections) or not 1 <= n <= 4:
+            raise ValueError(f"sections must be the pairs of 1 to 4 axes, got {sections}")
+        axes = b"".join(b"\0\1\2\3"[a:a + 1] * x for a, x in enumerate(sections))
     if len(axes) != half:
         raise ValueError(f"sections must cover the {half} pairs, got {len(axes)}")
-    return axes, n
+    return axes if n > 1 else None, n
 
 
 def _rotary(positions, inv_freq, sections, interleaved: bool, T: int, D: int):
-    """The quarot_rotary of a call, and the host array that it points to."""
+    """The quarot_rotary of a call (it keeps the host array that it points to)."""
     _ndim(inv_freq, 1, "inv_freq")
     half = inv_freq.shape[0]
     if 2 * half > D:
         raise ValueError(f"inv_freq must hold at most {D // 2} elements, got {half}")
     axes, n = _sections(sections, half)
-    stride = T
+    stride, at = T, None
     if positions is not None:
-        if positions.dim() == 1:
-            positions = positions[None]
-        _ndim(positions, 2, "positions")
-        if positions.shape[0] < n or positions.shape[1] < T:
+        shape, st = positions.shape, positions.stride()
+        if len(shape) == 1:
+            shape, st = (1, shape[0]), (T, st[0])
+        elif len(shape) != 2:
+            _ndim(positions, 2, "positions")
+        if shape[0] < n or shape[1] < T:
             raise ValueError(f"positions must have shape {(n, T)}, got {tuple(positions.shape)}")
-        n = positions.shape[0]
+        n = shape[0]
         if positions.dtype != torch.int32:
             raise TypeError(f"positions must be {torch.int32}, got {positions.dtype}")
         if not positions.is_cuda:
             raise ValueError("positions must be a device tensor")
-        if T > 1 and positions.stride(1) != 1:
+        if T > 1 and st[1] != 1:
             raise ValueError("positions must be contiguous along the tokens")
         if n > 1:
-            stride = positions.stride(0)
-    host = (ctypes.c_uint8 * half)(*axes) if axes is not None else None
-    r = _Rotary(positions.data_ptr() if positions is not None else None, stride,
-                _ptr(inv_freq, torch.float32, "inv_freq"),
-                ctypes.cast(host, _P) if host is not None else None, n, 2 * half,
-                int(bool(interleaved)))
-    return r, host
+            stride = st[0]
+        at = positions.data_ptr()
+    r = _Rotary(at, stride, _ptr(inv_freq, torch.float32, "inv_freq"),
+                ctypes.cast(axes, _P) if axes is not None else None, n, 2 * half,
+                1 if interleaved else 0)
+    r.axes = axes
+    return r
 
 
 def _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group: int, rows: torch.Tensor,
@@ -1015,7 +1020,7 @@ def quarot_rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor
     _half_rows(x, "x")
     _shape(y, x.shape, "y")
     T, H, D = x.shape
-    r, host = _rotary(positions, inv_freq, sections, interleaved, T, D)
+    r = _rotary(positions, inv_freq, sections, interleaved, T, D)
     _on_device(x.device, positions=positions, inv_freq=inv_freq, y=y)
     if y is None:
         y = torch.empty((T, H, D), dtype=torch.float16, device=x.device)
@@ -1056,7 +1061,7 @@ def quarot_kv_append_paged(k: torch.Tensor, v: torch.Tensor, k_cache, v_cache,
     cache = _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group, k, "k", True)
     r = None
     if inv_freq is not None:
-        r, host = _rotary(positions, inv_freq, sections, interleaved, T, D)
+        r = _rotary(positions, inv_freq, sections, interleaved, T, D)
     _on_device(k_cache[0].device, k=k, v=v, q=q, q_out=q_out, positions=positions,
                inv_freq=inv_freq)
     if q is not None and q_out is None:
