@@ -85,6 +85,24 @@ __device__ __forceinline__ int64_t pool_row(const PagedMap &m, int hkv, int b, i
     return in && (uint32_t)page < (uint32_t)m.n_pages ? row : -1;
 }
 
+// The 64 sequences or fewer, from lo on, that the last one of which before(b, cu[b])
+// holds is among (it holds up to some b): a 64-way search of cu, one load's latency
+// for each power of 64.  Each wave does it for itself.
+template <class Before>
+__device__ __forceinline__ void search(const PagedMap &m, int &lo, int &n, Before before)
+{
+    const int lane = threadIdx.x & 63;
+    lo = 0;
+    n = m.B;
+    while (n > 64) {
+        const int step = (n + 63) / 64, b = lo + min(lane * step, n - 1);
+        const uint64_t held = __ballot(lane * step < n && before(b, m.cu[b]));
+        const int i = held ? 63 - __builtin_clzll(held) : 0;
+        lo += i * step;
+        n = min(step, n - i * step);
+    }
+}
+
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
 hipError_t launch_paged_attention(const PagedAttnArgs &a, int rows, hipStream_t s);
 

@@ -57,31 +57,47 @@ __global__ __launch_bounds__(AP_THREADS) void k_rope_append(AppendArgs a)
     constexpr int LOGL = D == 64 ? 3 : D == 128 ? 4 : 5;
     constexpr int RPP = AP_THREADS / L;      // rows per pass
     __shared__ float2 cs[D / 2];
-    __shared__ int seq;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t t = blockIdx.x;
     const int pos = lane_pos(lane) & (L - 1);
+
+    // Row h of the token (the queries', keys', values' heads in turn), and for the
+    // halves' pairs its other half.  A row is read a pass ahead, the first one
+    // before anything is known of the token's sequence.
+    const RopeArgs &ro = a.rope;
+    const int heads = APPEND ? a.hq + 2 * a.hkv : a.hq, e0 = pos * 8;
+    const bool in_rot = e0 < 2 * ro.half, low = e0 < ro.half;
+    uint4 next, next_o = {};
+    auto fetch = [&](int h) {
+        const uint16_t *x = a.q + t * a.q_stride + h * D;
+        if (APPEND && h >= a.hq)
+            x = h >= a.hq + a.hkv ? a.v + t * a.v_stride + (h - a.hq - a.hkv) * D
+                                  : a.k + t * a.k_stride + (h - a.hq) * D;
+        next = *reinterpret_cast<const uint4 *>(x + e0);
+        if (in_rot && !ro.interleaved && (!APPEND || h < a.hq + a.hkv))
+            next_o = *reinterpret_cast<const uint4 *>(x + (low ? e0 + ro.half : e0 - ro.half));
+    };
+    const int h0 = blockIdx.y * RPP + tid / L;
+    if (h0 < heads)
+        fetch(h0);
 
     // the token's sequence and its slot in the pools (row of head 0, or -1)
     int at = (int)t;
     int64_t slot = -1;
     if constexpr (APPEND) {
         const PagedMap &m = a.map;
-        if (tid == 0)
-            seq = -1;
-        __syncthreads();
-        for (int b = tid; b < m.B; b += AP_THREADS)
-            if (m.cu[b] <= (int)t && (int)t < m.cu[b + 1])
-                seq = b;
-        __syncthreads();
-        const int b = seq;
-        if (b < 0)
+        int lo, n;
+        search(m, lo, n, [&](int, int cu) { return cu <= (int)t; });
+        const int bl = lo + min(lane, n - 1), c0 = m.cu[bl], c1 = m.cu[bl + 1], len = m.len[bl];
+        const uint64_t mine = __ballot(c0 <= (int)t && (int)t < c1);
+        if (mine == 0)
             return;
-        at = (int)((uint32_t)m.len[b] - (uint32_t)(m.cu[b + 1] - (int)t));
+        const int i = __builtin_ctzll(mine), b = lo + i;
+        at = (int)((uint32_t)__builtin_amdgcn_readlane(len, i) -
+                   (uint32_t)(__builtin_amdgcn_readlane(c1, i) - (int)t));
         slot = pool_row(m, a.hkv, b, at);
     }
 
-    const RopeArgs &ro = a.rope;
     if (tid < ro.half) {
         const int ax = (ro.axis[tid >> 4] >> (2 * (tid & 15))) & 3;
         const int p = ro.pos ? ro.pos[ax * ro.pos_stride + t] : at;
@@ -89,19 +105,17 @@ __global__ __launch_bounds__(AP_THREADS) void k_rope_append(AppendArgs a)
     }
     __syncthreads();
 
-    const int heads = APPEND ? a.hq + 2 * a.hkv : a.hq;
-    for (int h = blockIdx.y * RPP + tid / L; h < heads; h += gridDim.y * RPP) {
+    for (int h = h0; h < heads; h += gridDim.y * RPP) {
+        const uint4 row_raw = next, other = next_o;
+        if (h + (int)gridDim.y * RPP < heads)
+            fetch(h + gridDim.y * RPP);
         const bool isq = h < a.hq, isv = APPEND && h >= a.hq + a.hkv;
         const int hh = isq ? h : isv ? h - a.hq - a.hkv : h - a.hq;
         if (!isq && slot < 0)
             continue;
-        const uint16_t *x = isq ? a.q + t * a.q_stride : isv ? a.v + t * a.v_stride
-                                                            : a.k + t * a.k_stride;
-        x += hh * D;
-        const int e0 = pos * 8;
         float v[8];
-        load8(x + e0, v);
-        if (!isv && e0 < 2 * ro.half) {
+        unpack8(row_raw, v);
+        if (!isv && in_rot) {
             if (ro.interleaved) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
@@ -111,12 +125,8 @@ __global__ __launch_bounds__(AP_THREADS) void k_rope_append(AppendArgs a)
                     v[e + 1] = q * w.x + p * w.y;
                 }
             } else {
-                // the pair's other half: 8 elements of this row, read again
-                // (a lane's stores come after all of its wave's loads, so the
-                // row may be rewritten in place)
-                const bool low = e0 < ro.half;
                 float o[8];
-                load8(x + (low ? e0 + ro.half : e0 - ro.half), o);
+                unpack8(other, o);
                 const float2 *w = cs + (low ? e0 : e0 - ro.half);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {

@@ -36,25 +36,6 @@ struct Work : paged::Span {
     int tok0;  // first batch row (new token) of the sequence
 };
 
-// The first sequences of a batch of which before(b, rows before b) <= slot holds, as
-// far as the 64 sequences that the last of them lies in: a 64-way search of cu, one
-// load's latency for each power of 64.  Each wave does it for itself.
-template <class Before>
-__device__ __forceinline__ void search(const PagedAttnArgs &a, int &lo, int &n, Before before)
-{
-    const PagedMap &m = a.map;
-    const int lane = threadIdx.x & 63;
-    lo = 0;
-    n = m.B;
-    while (n > 64) {
-        const int step = (n + 63) / 64, b = lo + min(lane * step, n - 1);
-        const uint64_t below = __ballot(lane * step < n && before(b, (int64_t)m.cu[b] * a.rep));
-        const int i = below ? 63 - __builtin_clzll(below) : 0;
-        lo += i * step;
-        n = min(step, n - i * step);
-    }
-}
-
 __device__ __forceinline__ Work make_work(const PagedAttnArgs &a, int b, int c0, int c1, int len,
                                           int64_t block, int mr)
 {
@@ -72,7 +53,7 @@ __device__ __forceinline__ Work find_work(const PagedAttnArgs &a, int slot)
 {
     const PagedMap &m = a.map;
     int lo, n;
-    search(a, lo, n, [&](int b, int64_t rows) { return paged::first_slot(rows, b, MR) <= slot; });
+    search(m, lo, n, [&](int b, int cu) { return paged::first_slot((int64_t)cu * a.rep, b, MR) <= slot; });
     const int b = lo + min((int)threadIdx.x & 63, n - 1);
     const int c0 = m.cu[b], c1 = m.cu[b + 1], len = m.len[b];
     const uint64_t mine = __ballot(paged::first_slot((int64_t)c0 * a.rep, b, MR) <= slot &&
@@ -99,7 +80,7 @@ __device__ __forceinline__ Work few_work(const PagedAttnArgs &a, int slot)
     int64_t rb = 0;
     if (extra >= 0) {
         int lo, n;
-        search(a, lo, n, [&](int, int64_t rows) { return rows / MR <= extra; });
+        search(m, lo, n, [&](int, int cu) { return (int64_t)cu * a.rep / MR <= extra; });
         const int64_t rows = (int64_t)m.cu[lo + min((int)threadIdx.x & 63, n - 1)] * a.rep;
         const uint64_t below = __ballot(((int)threadIdx.x & 63) < n && rows / MR <= extra);
         if (below == 0)

@@ -62,15 +62,19 @@ __device__ __forceinline__ uint32_t asym_code_bits(float y, const Divisor &d, fl
     return round_bits(fminf(fmaxf(quotient(y - zf, d), 0.0f), 15.0f));
 }
 
-__device__ __forceinline__ void load8(const uint16_t *p, float *v)
+__device__ __forceinline__ void unpack8(uint4 raw, float *v)
 {
-    uint4 raw = *reinterpret_cast<const uint4 *>(p);
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[2 * i] = h2f((uint16_t)(w[i] & 0xFFFFu));
         v[2 * i + 1] = h2f((uint16_t)(w[i] >> 16));
     }
+}
+
+__device__ __forceinline__ void load8(const uint16_t *p, float *v)
+{
+    unpack8(*reinterpret_cast<const uint4 *>(p), v);
 }
 
 __device__ __forceinline__ void store8(uint16_t *p, const float *v)
