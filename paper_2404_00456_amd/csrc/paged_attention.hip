@@ -403,7 +403,7 @@ __global__ __launch_bounds__(64 * NW)
     constexpr int KS = D / 16, DB = D / 32;
     // A stage holds 64 tokens (32 for D = 256).  While one's scores are taken and
     // the last one's values are added, the next but one is written.
-    constexpr int TS = D == 256 ? 32 : 64, NB = D == 256 ? 4 : 3;
+    constexpr int TS = D == 256 || NW == 2 ? 32 : 64, NB = TS == 32 ? 4 : 3;
     using St = Stage<D, TS>;
     using Sh = Share<D, TS, NT>;
     __shared__ __align__(16) St st[NB];

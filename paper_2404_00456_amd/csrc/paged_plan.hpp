@@ -148,12 +148,17 @@ inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
     return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
 }
 
+// Tiles: 256 blocks, one a CU as LDS holds them (two of the 64-row tile): a second
+// turn of blocks costs more than the joining of fewer splits saves (512 new tokens
+// over 16384, 64 heads on 8: 319 us in 256 blocks, 329 in 512; 4 x 64 over 8192: 70
+// and 101; single tokens over 8192 in groups of 32, 64-row tiles: 142 us in 512
+// blocks, 223 in 256).
 inline Part tile_part(Which which, int64_t steps, int64_t rows, int64_t T, int64_t B, int64_t hkv,
                       int64_t rep, int64_t D)
 {
     Part p{which, D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256, 1, 4};
     const int64_t blocks = hkv * std::max<int64_t>((T * rep + p.rows - 1) / p.rows, which == MANY ? 1 : B);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, 512 / blocks, 128,
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, (p.rows == 64 ? 512 : 256) / blocks, 128,
                                                             2048 / (hkv * slots(p, T, B, rep))}));
     return p;
 }
