@@ -523,8 +523,9 @@ quarot_status quarot_kv_decode_attention(const quarot_f16 *q, const uint8_t *k_c
  * next tokens of all of them to each layer at once.  These calls take such a
  * batch: T token rows, of which rows cu_new[b] .. cu_new[b + 1] - 1 are the new
  * tokens of sequence b (none, one, or a chunk of a prompt), in order.  Rows
- * from cu_new[batch] on belong to nobody: they are neither read nor written,
- * so that a captured graph can serve batches of up to T tokens.
+ * from cu_new[batch] on belong to nobody: nothing comes of them and nothing is
+ * written for them, so that a captured graph can serve batches of up to T
+ * tokens.
  *
  * Rotary positions (in the attention block of §4 Stage 1d they come before the
  * head-wise Hadamard).  Pair f < rot_dim / 2 of a head row is the elements
@@ -637,7 +638,8 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
  * max_seq_len >= 1: the longest seq_lens to plan for (a longer one is right as
  * well, only slower).  workspace: quarot_kv_paged_attention_workspace_size
  * bytes, 16-byte aligned, may be NULL when that is 0; every call writes what it
- * reads of it.  One or two launches.
+ * reads of it, and calls that may run at the same time need one each.  Four
+ * launches at most (long and short sequences apart, and the joining of each).
  */
 quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, quarot_f16 *out,
                                         int64_t out_stride, const quarot_paged_kv *cache, int64_t T,

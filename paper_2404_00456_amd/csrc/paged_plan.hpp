@@ -140,11 +140,11 @@ QUAROT_HD int64_t part_row(Which which, int64_t b, int64_t tok0, int64_t rep)
 // of 1 .. 2048 tokens: 97 and 75), longer ones leave CUs idle behind the longest
 // (64 of 1 .. 8192: 73 us in splits of 32 steps, 89 of 64), and few steps do best
 // in pieces of 4 (one of 4096: 10.5 us, 13 of 8, 21 of 24; but one of 32768: 22 of
-// 4, 19 of 8).
+// 4, 19 of 8).  8192 blocks at most, which bounds the workspace as well.
 inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
 {
     const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * B * hkv / 512));
-    const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, (1 << 20) / (B * hkv)});
+    const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, 8192 / (B * hkv)});
     return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
 }
 
@@ -158,8 +158,10 @@ inline Part tile_part(Which which, int64_t steps, int64_t rows, int64_t T, int64
 {
     Part p{which, D == 256 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256, 1, 4};
     const int64_t blocks = hkv * std::max<int64_t>((T * rep + p.rows - 1) / p.rows, which == MANY ? 1 : B);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, (p.rows == 64 ? 512 : 256) / blocks, 128,
-                                                            2048 / (hkv * slots(p, T, B, rep))}));
+    const int64_t fill = (p.rows == 64 ? 512 : 256) / blocks;
+    // (slots that no sequence fills cost a start each)
+    const int64_t most = 2048 / (hkv * slots(p, T, B, rep));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(steps + 3) / 4, fill, most, 128}));
     return p;
 }
 
@@ -176,7 +178,7 @@ inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int6
     const int64_t steps = (seen + STEP - 1) / STEP;
     if (G != D || rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
         return Plan{1, {tile_part(ALL, steps, rows, T, B, hkv, rep, D)}};
-    if (rows <= FEW_ROWS && most <= 4 * FEW_ROWS)
+    if (rows <= FEW_ROWS && most <= 4 * FEW_ROWS)  // no long sequence among them
         return Plan{1, {few_part(ALL, steps, B, hkv)}};
     return Plan{2, {tile_part(MANY, steps, std::max(rows, most / 4), T, B, hkv, rep, D),
                     few_part(FEW, steps, B, hkv)}};

@@ -445,3 +445,115 @@ def test_two_streams_at_once(dev, orc):
         assert err <= tol
         for o in outs[1:]:
             assert torch.equal(o, outs[0])
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 30, 17]])
+@pytest.mark.parametrize("D,hkv", [(128, 2), (64, 4), (256, 1)])
+def test_zero_scales(dev, orc, new, D, hkv):
+    """Rows of equal values have a scale of 0 and are their zero: some tokens of
+    each sequence, all of the last."""
+    bt = Batch(31, new, [200, 130, 77], hkv, D, D, 16)
+    for pool in (bt.k, bt.v):
+        for b, page in enumerate(bt.table):
+            for i, pg in enumerate(page):
+                if pg >= 0:
+                    held = bt.held[pg] & (np.arange(16) % 3 == 0 if b < 2 else True)
+                    pool[1][pg][:, held] = 0
+    check(dev, orc, bt, 4 * hkv)
+
+
+def test_two_graphs_share_a_workspace(dev, orc):
+    """A decode step and a mixed batch, captured with the same workspace and
+    replayed in turn for other lengths."""
+    import torch
+    import paper_2404_00456_amd as q
+    H, hkv, D = 16, 2, 128
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device=dev)
+    stream, runs = torch.cuda.Stream(), []
+    for new, total in (([1, 1, 1], [5000, 3001, 64]), ([1, 70, 0, 2], [4100, 3000, 9, 2222])):
+        bt = Batch(40 + len(new), new, total, hkv, D, D, 64, behind=3)
+        qh = bt.queries(H)
+        assert 0 < q.quarot_kv_paged_attention_workspace_size(bt.T, len(new), H, hkv, D, 5000) <= 1 << 24
+        d = [D_(a, dev) for a in (qh, *bt.k, *bt.v, bt.table, bt.lens, bt.cu)]
+        out = torch.zeros(qh.shape, dtype=torch.float16, device=dev)
+
+        def step(d=d, out=out):
+            q.quarot_kv_paged_attention(d[0], d[1:4], d[4:7], *d[7:], max_seq_len=5000, out=out,
+                                        workspace=ws)
+        with torch.cuda.stream(stream):
+            step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        runs.append((bt, qh, d, out, graph))
+    for k in range(4):
+        for bt, qh, d, out, graph in runs:
+            lens = np.maximum(bt.lens - 37 * k, np.diff(bt.cu)).astype(np.int32)
+            d[8].copy_(D_(lens, dev))
+            out.fill_(9.0)
+            (d[0].float() @ d[0].float().transpose(1, 2)).sum().item()  # other work between
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.cpu().numpy()
+            ref = orc.paged_attention(qh, bt.k, bt.v, bt.table, lens, bt.cu, D,
+                                      out=np.full(qh.shape, 9.0))
+            assert (got[bt.cu[-1]:] == 9.0).all()
+            assert np.abs(got - ref).max() <= attention_tolerance(bt, qh, True)
+
+
+def test_pools_past_32_bits(dev, orc):
+    """Pages whose offsets pass 2^32 bytes hold and give what the same pages do at
+    the front of a small pool."""
+    import torch
+    import paper_2404_00456_amd as q
+    hkv, D, G, page = 2, 256, 32, 64
+    bt = Batch(50, [1, 40], [150, 300], hkv, D, G, page, exact=False)
+    per = hkv * page * D // 2
+    shift = (1 << 32) // per + 3
+    far = bt.table + np.where(bt.table >= 0, shift, 0).astype(np.int32)
+    x = torch.randn(bt.T, 4 * hkv, D, device=dev).half()
+    results = []
+    for table, pages in ((bt.table, bt.pages), (far, bt.pages + shift)):
+        pools = []
+        for pool in (bt.k, bt.v):
+            big = [torch.empty((pages,) + a.shape[1:], dtype=torch.from_numpy(a).dtype, device=dev)
+                   for a in pool]
+            for t, a in zip(big, pool):
+                t[pages - bt.pages:] = D_(a, dev)
+            pools.append(tuple(big))
+        rest = (D_(table, dev), D_(bt.lens, dev), D_(bt.cu, dev))
+        q.quarot_kv_append_paged(x[:, :hkv], x[:, hkv:2 * hkv], *pools, *rest, group=G)
+        results.append([t[pages - bt.pages:].clone() for p in pools for t in p] +
+                       [q.quarot_kv_paged_attention(x, *pools, *rest, group=G),
+                        q.quarot_kv_paged_attention(x[:1], *pools, *(t[:1] for t in rest[:2]),
+                                                    rest[2][:2], group=G)])
+        del pools, big
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert not torch.equal(results[0][0], D_(bt.k[0], dev))  # the new tokens were stored
+
+
+@pytest.mark.parametrize("G", [128, 32])
+def test_one_group_pools_past_32_bits(dev, orc, G):
+    """The same for the kernel of single tokens (one group a row)."""
+    import torch
+    import paper_2404_00456_amd as q
+    hkv, D, page = 1, 128, 16
+    bt = Batch(51, [1, 1], [100, 37], hkv, D, G, page)
+    shift = (1 << 32) // (hkv * page * D // 2) + 1
+    qh = D_(bt.queries(8), dev)
+    outs = []
+    for off in (0, shift):
+        pools = []
+        for pool in (bt.k, bt.v):
+            big = [torch.empty((bt.pages + off,) + a.shape[1:], dtype=torch.from_numpy(a).dtype,
+                               device=dev) for a in pool]
+            for t, a in zip(big, pool):
+                t[off:] = D_(a, dev)
+            pools.append(tuple(big))
+        table = bt.table + np.where(bt.table >= 0, off, 0).astype(np.int32)
+        outs.append(q.quarot_kv_paged_attention(qh, *pools, D_(table, dev), D_(bt.lens, dev),
+                                                D_(bt.cu, dev), group=G))
+        del pools, big
+    assert torch.equal(outs[0], outs[1])
