@@ -1,0 +1,169 @@
+// Drives the host code of the rotary and paged entry points with no device:
+// argument validation (null, negative, oversized and misaligned arguments,
+// extreme sizes), the no-device path of valid calls and the workspace query.
+// Built with the address and undefined-behaviour sanitizers by
+// tests/test_paged_host.py against counting stand-ins of the kernel launchers.
+#include <cstdint>
+#include <cstdio>
+
+#include "../../paper_2404_00456_amd/csrc/paged.hpp"
+#include "quarot.h"
+
+extern int quarot_stub_launches;  // tests/native/launch_stubs.cpp
+
+namespace quarot {
+
+hipError_t launch_append(const AppendArgs &, hipStream_t)
+{
+    ++quarot_stub_launches;
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_attention(const PagedAttnArgs &, int, hipStream_t)
+{
+    ++quarot_stub_launches;
+    return hipErrorInvalidValue;
+}
+
+}  // namespace quarot
+
+static int failures = 0;
+
+#define EXPECT(call, want)                                                                   \
+    do {                                                                                     \
+        const long long got_ = (long long)(call);                                            \
+        if (got_ != (long long)(want)) {                                                     \
+            std::printf("FAIL line %d: %s -> %lld, want %lld\n", __LINE__, #call, got_,      \
+                        (long long)(want));                                                  \
+            ++failures;                                                                      \
+        }                                                                                    \
+    } while (0)
+
+int main()
+{
+    void *P = reinterpret_cast<void *>(uintptr_t(1) << 20);
+    quarot_f16 *H = static_cast<quarot_f16 *>(P);
+    quarot_f16 *O = reinterpret_cast<quarot_f16 *>((uintptr_t(1) << 20) + 4096);
+    quarot_f16 *U = reinterpret_cast<quarot_f16 *>((uintptr_t(1) << 20) + 8);
+    uint8_t *C = static_cast<uint8_t *>(P);
+    int32_t *I = static_cast<int32_t *>(P);
+    float *F = static_cast<float *>(P);
+    const int64_t BIG = INT64_MAX, M = INT64_MIN;
+    uint8_t axes[64] = {};
+
+    const quarot_rotary rot = {I, 16, F, axes, 1, 128, 0};
+    auto rope = [&](quarot_rotary r, int64_t T = 8, int64_t H_ = 4, int64_t D = 128, int64_t xs = 512,
+                    int64_t ys = 512, quarot_f16 *x = nullptr, quarot_f16 *y = nullptr) {
+        return quarot_rope(x ? x : H, xs, y ? y : O, ys, &r, T, H_, D, 1, nullptr);
+    };
+    EXPECT(rope(rot), QUAROT_ERR_NO_DEVICE);
+    EXPECT(rope(rot, 0), QUAROT_OK);
+    EXPECT(quarot_rope(H, 512, O, 512, nullptr, 8, 4, 128, 1, nullptr), QUAROT_ERR_INVALID_ARG);
+    EXPECT(quarot_rope(nullptr, 512, O, 512, &rot, 8, 4, 128, 1, nullptr), QUAROT_ERR_INVALID_ARG);
+    for (int64_t bad : {M, int64_t(-1), BIG}) {
+        EXPECT(rope(rot, bad) != QUAROT_OK, 1);
+        EXPECT(rope(rot, 8, bad) != QUAROT_OK, 1);
+        EXPECT(rope(rot, 8, 4, bad) != QUAROT_OK, 1);
+        EXPECT(rope(rot, 8, 4, 128, bad) != QUAROT_OK, 1);
+        EXPECT(rope(rot, 8, 4, 128, 512, bad) != QUAROT_OK, 1);
+        quarot_rotary r = rot;
+        r.pos_stride = bad;
+        EXPECT(rope(r) != QUAROT_OK, 1);
+    }
+    EXPECT(rope(rot, 8, 4, 128, 516), QUAROT_ERR_ALIGNMENT);
+    EXPECT(rope(rot, 8, 4, 128, 512, 512, U), QUAROT_ERR_ALIGNMENT);
+    EXPECT(rope(rot, 8, 4, 128, 512, 520, H, H), QUAROT_ERR_INVALID_ARG);
+    EXPECT(rope(rot, 8, 4, 96, 512), QUAROT_ERR_UNSUPPORTED_SIZE);
+    for (int n : {INT32_MIN, -1, 0, 5, INT32_MAX}) {
+        quarot_rotary r = rot;
+        r.n_axes = n;
+        EXPECT(rope(r) != QUAROT_OK, 1);
+        r = rot;
+        r.rot_dim = n;
+        EXPECT(rope(r) != QUAROT_OK, 1);
+    }
+    axes[63] = 1;
+    EXPECT(rope(rot), QUAROT_ERR_INVALID_ARG);
+    quarot_rotary two = rot;
+    two.n_axes = 2;
+    EXPECT(rope(two), QUAROT_ERR_NO_DEVICE);
+    axes[63] = 0;
+
+    const quarot_paged_kv kv = {C, H, H, C, H, H, I, I, I, 4, 2, 128, 128, 64, 64, 32};
+    auto append = [&](quarot_paged_kv c, int64_t T = 8, int64_t nh = 4, int64_t st = 512,
+                      float clip = 0.95f) {
+        return quarot_kv_append_paged(nh ? H : nullptr, st, nh ? O : nullptr, st, H, 256, H, 256, &c, &rot,
+                                      T, nh, 1, 0, clip, nullptr);
+    };
+    auto attend = [&](quarot_paged_kv c, int64_t T = 8, int64_t nh = 4, int64_t st = 512,
+                      int64_t most = 2048, int64_t window = 0, int64_t sinks = 0, float scale = 0.1f,
+                      void *ws = nullptr, size_t bytes = 0) {
+        return quarot_kv_paged_attention(H, st, O, st, &c, T, nh, most, window, sinks, scale, ws, bytes,
+                                         nullptr);
+    };
+    EXPECT(append(kv), QUAROT_ERR_NO_DEVICE);
+    EXPECT(append(kv, 8, 0), QUAROT_ERR_NO_DEVICE);
+    EXPECT(append(kv, 0), QUAROT_OK);
+    EXPECT(append(kv, 8, 4, 512, 0.0f), QUAROT_ERR_INVALID_ARG);
+    EXPECT(attend(kv, 0), QUAROT_OK);
+    EXPECT(attend(kv, 8, 3), QUAROT_ERR_INVALID_ARG);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, 0.0f), QUAROT_ERR_INVALID_ARG);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, __builtin_inff()), QUAROT_ERR_INVALID_ARG);
+    EXPECT(attend(kv, 8, 4, 512, 2048, -1), QUAROT_ERR_INVALID_ARG);
+    EXPECT(attend(kv, 8, 4, 512, 0), QUAROT_ERR_INVALID_ARG);
+    const size_t need = quarot_kv_paged_attention_workspace_size(8, 4, 4, 2, 128, 128, 2048, 0, 0);
+    EXPECT(need > 0, 1);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, 0.1f, P, need - 1), QUAROT_ERR_WORKSPACE);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, 0.1f, nullptr, need), QUAROT_ERR_WORKSPACE);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, 0.1f, U, need), QUAROT_ERR_ALIGNMENT);
+    EXPECT(attend(kv, 8, 4, 512, 2048, 0, 0, 0.1f, P, need), QUAROT_ERR_NO_DEVICE);
+    // one field of the cache at a time
+    for (int field = 0; field < 7; ++field)
+        for (int64_t bad : {M, int64_t(-1), int64_t(0), BIG, int64_t(1) << 40}) {
+            quarot_paged_kv c = kv;
+            int64_t *f[] = {&c.batch, &c.n_kv_heads, &c.head_dim, &c.group, &c.n_pages, &c.page_size,
+                            &c.max_pages};
+            *f[field] = bad;
+            EXPECT(append(c) != QUAROT_OK && append(c) != QUAROT_ERR_NO_DEVICE, 1);
+            EXPECT(attend(c, 8, 4, 512, 2048, 0, 0, 0.1f, P, SIZE_MAX) != QUAROT_ERR_NO_DEVICE, 1);
+        }
+    for (int field = 0; field < 9; ++field)
+        for (uintptr_t at : {uintptr_t(0), (uintptr_t(1) << 20) + 2}) {
+            quarot_paged_kv c = kv;
+            void **f = reinterpret_cast<void **>(&c) + field;
+            *f = reinterpret_cast<void *>(at);
+            const int want = at ? QUAROT_ERR_ALIGNMENT : QUAROT_ERR_INVALID_ARG;
+            EXPECT(append(c), want);
+            EXPECT(attend(c), want);
+        }
+    for (int64_t bad : {M, int64_t(-1), BIG, int64_t(1) << 31}) {
+        EXPECT(append(kv, bad) != QUAROT_OK && append(kv, bad) != QUAROT_ERR_NO_DEVICE, 1);
+        EXPECT(append(kv, 8, bad) != QUAROT_OK && append(kv, 8, bad) != QUAROT_ERR_NO_DEVICE, 1);
+        EXPECT(attend(kv, bad) != QUAROT_OK, 1);
+        EXPECT(attend(kv, 8, bad) != QUAROT_OK, 1);
+    }
+    // extreme sizes of the queries and of the workspace
+    for (int64_t T : {int64_t(1), int64_t(8), int64_t(1) << 20, int64_t(1) << 30, BIG})
+        for (int64_t B : {int64_t(1), int64_t(64), int64_t(0xFFFFFF), BIG})
+            for (int64_t hq : {int64_t(1), int64_t(64), int64_t(0xFFFF)})
+                for (int64_t most : {int64_t(1), int64_t(4096), BIG})
+                    for (int64_t window : {int64_t(0), int64_t(1), BIG})
+                        for (int64_t D : {64, 128, 256}) {
+                            const size_t n = quarot_kv_paged_attention_workspace_size(
+                                T, B, hq, 1, D, D, most, window, BIG);
+                            // partial results stay small beside the caches they join
+                            if (T <= 1 << 20 && B <= 1 << 20 && hq <= 64)
+                                EXPECT(n <= size_t(1) << 31, 1);
+                        }
+    EXPECT(quarot_kv_paged_attention_workspace_size(8, 4, 4, 3, 128, 128, 2048, 0, 0), 0);
+    EXPECT(quarot_kv_paged_attention_workspace_size(-1, 4, 4, 2, 128, 128, 2048, 0, 0), 0);
+    EXPECT(quarot_kv_paged_attention_workspace_size(8, 4, 4, 2, 100, 100, 2048, 0, 0), 0);
+
+    EXPECT(quarot_stub_launches, 0);  // nothing tried to launch
+    if (failures) {
+        std::printf("%d failure(s)\n", failures);
+        return 1;
+    }
+    std::printf("ok\n");
+    return 0;
+}

@@ -346,3 +346,29 @@ def test_binding_refuses_types():
         q.quarot_rope(torch.zeros(4, 2, 128), i32(4), FREQ)
     with pytest.raises(TypeError):
         q.quarot_rope(f16(4, 2, 128), torch.zeros(4, dtype=torch.int64), FREQ)
+
+
+def test_host_code_under_asan_ubsan():
+    """The entry points' host code under both sanitizers, with no device, against
+    counting stand-ins of the launchers (tests/native/paged_abi_check.cpp)."""
+    import test_sanitizers as ts
+    if not os.path.exists(ts.HIPCC) or ts.clang_asan_runtime() is None:
+        pytest.skip("needs hipcc and clang's ASan runtime")
+    csrc, native = (os.path.join(ROOT, *p) for p in (("paper_2404_00456_amd", "csrc"),
+                                                     ("tests", "native")))
+    san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+           "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host",
+           "-fno-omit-frame-pointer"]
+    with tempfile.TemporaryDirectory() as d:
+        exe = os.path.join(d, "paged_abi_check")
+        subprocess.run([ts.HIPCC, "-O1", "-g", "-std=c++17", *san, "-I", os.path.join(ROOT, "include"),
+                        *(os.path.join(csrc, f) for f in ("capi.cpp", "capi_paged.cpp",
+                                                          "host_rules.cpp")),
+                        *(os.path.join(native, f) for f in ("launch_stubs.cpp",
+                                                            "paged_abi_check.cpp")), "-o", exe],
+                       check=True, capture_output=True, timeout=600)
+        env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1",
+                   HIP_VISIBLE_DEVICES="-1")
+        res = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+        assert res.returncode == 0 and res.stdout.strip().endswith("ok"), \
+            res.stdout[-3000:] + res.stderr[-3000:]
