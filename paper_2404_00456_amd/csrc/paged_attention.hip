@@ -10,11 +10,24 @@
 // k_paged_tile: a block takes 32 rows per wave and walks over the tokens that
 // any of them sees, 64 at a time.  The codes of a step become fp16 values in
 // LDS (RN16 of code * scale + zero, one rounding, as quarot_kv_dequant gives
-// them; half an fp16 step of a key or value is what the fp16 output keeps of
-// it as well).  Scores are taken transposed, S = K Q^T, so that the lane that
-// holds a query's scores also holds its share of the weights as the B operand
-// of O = V^T P^T: the weights never leave their registers.  Softmax sums and
-// outputs are binary32; weights are rounded to fp16 for the product.
+// them), once for all waves.  Scores are taken transposed, S = K Q^T, so that
+// the lane that holds a query's scores also holds its share of the weights as the
+// B operand of O = V^T P^T: the weights never leave their registers.  Softmax
+// sums and outputs are binary32.  Three roundings to fp16 come on top of the
+// output's own: keys, values, and weights for their product.  Each is off by half
+// a step at most and at random, so that an output of many tokens is off by about
+// 5e-4 of its size instead of 2e-4; taking the codes as they are and the weights
+// in two parts, as k_paged_rows does, would be half as many matrix products again
+// where these are what bounds the kernel.
+//
+// What bounds it: 32 rows by 32 tokens by 128 dimensions are 16 matrix
+// instructions of 32 cycles, about 115 vector instructions (softmax 60, staging
+// 40) and 18 KB of LDS traffic, each about half of a SIMD's time when two waves
+// share it, so all three have to run beside each other.  8192 tokens of 64 heads
+// on 8 take 1.14 to 1.24 ms by the card's clock, 890 .. 970 TFLOP/s where a
+// library product of 8192^3 reaches 1330.  One wave with 64 rows a SIMD (half the
+// LDS reads) was slower, 1.78 ms: its 512 registers are half accumulators, and
+// the softmax works through copies of them.
 #include <algorithm>
 
 #include "lds_dma.hpp"
@@ -175,7 +188,8 @@ struct Stage {
     }
 };
 
-// What a thread stages of TS tokens: N items of EK elements of a key, and N items
+// What a thread stages of TS tokens (by roles, half of the waves the keys and half
+// the values, a prompt of 8192 took 1.25 ms, 1.20 so): N items of EK elements of a key, and N items
 // of DV elements of four tokens' values.  Every thread has some of both, so that
 // no step carries a branch, and the items come to pieces of a pair of values each,
 // which the main loop spreads between its matrix products.  The items of a wave
@@ -401,7 +415,8 @@ __global__ __launch_bounds__(64 * NW)
 {
     constexpr int NT = 64 * NW, MR = 32 * NW;
     constexpr int KS = D / 16, DB = D / 32;
-    // A stage holds 64 tokens (32 for D = 256).  While one's scores are taken and
+    // A stage holds 64 tokens, 32 for D = 256 and for two waves, of which then two
+    // blocks fit a CU (single tokens over 8192 in groups of 32: 197 us with 64).  While one's scores are taken and
     // the last one's values are added, the next but one is written.
     constexpr int TS = D == 256 || NW == 2 ? 32 : 64, NB = TS == 32 ? 4 : 3;
     using St = Stage<D, TS>;

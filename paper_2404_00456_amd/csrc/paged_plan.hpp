@@ -143,7 +143,7 @@ QUAROT_HD int64_t part_row(Which which, int64_t b, int64_t tok0, int64_t rep)
 // 4, 19 of 8).  8192 blocks at most, which bounds the workspace as well.
 inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
 {
-    const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * B * hkv / 512));
+    const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * std::min<int64_t>(B * hkv, 1 << 20) / 512));
     const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, 8192 / (B * hkv)});
     return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
 }
@@ -178,8 +178,14 @@ inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int6
     const int64_t steps = (seen + STEP - 1) / STEP;
     if (G != D || rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
         return Plan{1, {tile_part(ALL, steps, rows, T, B, hkv, rep, D)}};
-    if (rows <= FEW_ROWS && most <= 4 * FEW_ROWS)  // no long sequence among them
+    // Sequences of few rows: guessed tokens of 64 sequences, 16 rows each, take 66 us
+    // so and 84 with a launch for longer ones beside; but a batch of single tokens
+    // may hold a chunk of all the rest, which the tiles read four times as fast, so
+    // only up to 1024 rows of it.
+    if (rows <= FEW_ROWS && most <= 64 * FEW_ROWS)
         return Plan{1, {few_part(ALL, steps, B, hkv)}};
+    // Chunks, with single tokens among them maybe: 64 sequences, half of them one
+    // token, 244 us so and 285 in tiles alone, where nothing but chunks loses 4 us.
     return Plan{2, {tile_part(MANY, steps, std::max(rows, most / 4), T, B, hkv, rep, D),
                     few_part(FEW, steps, B, hkv)}};
 }
