@@ -990,23 +990,28 @@ def _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group: int, rows: 
     _ndim(kc, 4, "k_codes")
     pages, heads, page, half = kc.shape
     _group(group, 2 * half)
-    _shape(vc, kc.shape, "v_codes")
     consts = (pages, heads, page, 2 * half // group)
-    for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
-        _shape(t, consts, nm)
     _ndim(page_table, 2, "page_table")
     B, most = page_table.shape
+    # in one go where all is as it should be, as in nearly every call
+    if not (vc.shape == kc.shape and ks.shape == kz.shape == vs.shape == vz.shape == consts):
+        _shape(vc, kc.shape, "v_codes")
+        for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
+            _shape(t, consts, nm)
     _shape(seq_lens, (B,), "seq_lens")
     _shape(cu_new, (B + 1,), "cu_new")
     _shape(rows, (rows.shape[0], heads if kv_rows else rows.shape[1], 2 * half), name)
-    _on_device(kc.device, k_scale=ks, k_zero=kz, v_codes=vc, v_scale=vs, v_zero=vz,
-               page_table=page_table, seq_lens=seq_lens, cu_new=cu_new)
-    f16, i32 = torch.float16, torch.int32
-    return _PagedKV(
-        _ptr(kc, torch.uint8, "k_codes"), _ptr(ks, f16, "k_scale"), _ptr(kz, f16, "k_zero"),
-        _ptr(vc, torch.uint8, "v_codes"), _ptr(vs, f16, "v_scale"), _ptr(vz, f16, "v_zero"),
-        _ptr(page_table, i32, "page_table"), _ptr(seq_lens, i32, "seq_lens"),
-        _ptr(cu_new, i32, "cu_new"), B, heads, 2 * half, group, pages, page, most)
+    u8, f16, i32 = torch.uint8, torch.float16, torch.int32
+    dev, at = kc.device, []
+    for t, dtype, nm in ((kc, u8, "k_codes"), (ks, f16, "k_scale"), (kz, f16, "k_zero"),
+                         (vc, u8, "v_codes"), (vs, f16, "v_scale"), (vz, f16, "v_zero"),
+                         (page_table, i32, "page_table"), (seq_lens, i32, "seq_lens"),
+                         (cu_new, i32, "cu_new")):
+        if t.device != dev:
+            raise ValueError(f"{nm} must be on {dev}, got {t.device}")
+        at.append(_ptr(t, dtype, nm))
+    _on_device(dev)
+    return _PagedKV(*at, B, heads, 2 * half, group, pages, page, most)
 
 
 def quarot_rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, sections=None,
