@@ -916,6 +916,15 @@ def _token_rows(t: torch.Tensor, name: str):
     return t.data_ptr(), st[0] if T > 1 else H * D
 
 
+def _new(shape, dtype, dev, stream: Optional[torch.cuda.Stream]):
+    """Memory for a call on `stream`, from that stream's own, so that it is not
+    in use elsewhere and, once let go, is not reused before the call is through."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
 def _on_device(dev, **tensors):
     """Every tensor on `dev`, and `dev` the current device (whose stream the
     call runs on)."""
@@ -1028,7 +1037,7 @@ def quarot_rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor
     r = _rotary(positions, inv_freq, sections, interleaved, T, D)
     _on_device(x.device, positions=positions, inv_freq=inv_freq, y=y)
     if y is None:
-        y = torch.empty((T, H, D), dtype=torch.float16, device=x.device)
+        y = _new((T, H, D), torch.float16, x.device, stream)
     (xp, xs), (yp, ys) = _token_rows(x, "x"), _token_rows(y, "y")
     _check("quarot_rope", lib().quarot_rope(
         xp, xs, yp, ys, ctypes.byref(r), T, H, D, int(bool(rotate)), _stream(stream)))
@@ -1070,7 +1079,7 @@ def quarot_kv_append_paged(k: torch.Tensor, v: torch.Tensor, k_cache, v_cache,
     _on_device(k_cache[0].device, k=k, v=v, q=q, q_out=q_out, positions=positions,
                inv_freq=inv_freq)
     if q is not None and q_out is None:
-        q_out = torch.empty((T, H, D), dtype=torch.float16, device=q.device)
+        q_out = _new((T, H, D), torch.float16, q.device, stream)
     qp = qs = op = os_ = None
     if q is not None:
         (qp, qs), (op, os_) = _token_rows(q, "q"), _token_rows(q_out, "q_out")
@@ -1115,13 +1124,13 @@ def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: tor
     if sm_scale is None:
         sm_scale = D ** -0.5
     if out is None:
-        out = torch.empty((T, H, D), dtype=torch.float16, device=q.device)
+        out = _new((T, H, D), torch.float16, q.device, stream)
     (qp, qs), (op, ost) = _token_rows(q, "q"), _token_rows(out, "out")
     if workspace is None:
         need = quarot_kv_paged_attention_workspace_size(
             T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks, group)
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = _new((need,), torch.uint8, q.device, stream)
     _check("quarot_kv_paged_attention", lib().quarot_kv_paged_attention(
         qp, qs, op, ost, ctypes.byref(cache), T, H, int(max_seq_len), int(window), int(n_sinks),
         float(sm_scale),

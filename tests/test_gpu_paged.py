@@ -557,3 +557,33 @@ def test_one_group_pools_past_32_bits(dev, orc, G):
                                                 D_(bt.cu, dev), group=G))
         del pools, big
     assert torch.equal(outs[0], outs[1])
+
+
+def test_memory_of_a_call_on_another_stream(dev, orc, monkeypatch):
+    """What a call on `stream` allocates is that stream's, not the current one's,
+    whose work may still use it or reuse it too soon."""
+    import torch
+    import paper_2404_00456_amd as q
+    bt = Batch(60, [1, 1], [3000, 500], 2, 128, 128, 64)
+    qh = D_(bt.queries(16), dev)
+    args = [D_(a, dev) for a in (*bt.k, *bt.v, bt.table, bt.lens, bt.cu)]
+    pos, fr = torch.zeros(2, dtype=torch.int32, device=dev), D_(freq(128), dev)
+    kv = torch.zeros(2, 2, 128, dtype=torch.float16, device=dev)
+    want = q.quarot_kv_paged_attention(qh, args[:3], args[3:6], *args[6:])
+    turned = q.quarot_rope(qh, pos, fr)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    on, empty = [], torch.empty
+
+    def spy(*a, **kw):
+        on.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **kw)
+
+    with monkeypatch.context() as m:
+        m.setattr(torch, "empty", spy)
+        outs = [q.quarot_kv_paged_attention(qh, args[:3], args[3:6], *args[6:], stream=side),
+                q.quarot_rope(qh, pos, fr, stream=side)]
+        q.quarot_kv_append_paged(kv, kv, args[:3], args[3:6], *args[6:], q=qh, stream=side)
+    assert len(on) == 4 and set(on) == {side.cuda_stream}
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], turned)
