@@ -41,7 +41,7 @@ quarot_status check_rotary(const quarot_rotary *r, int64_t T, int64_t D, bool ow
         return QUAROT_ERR_INVALID_ARG;
     if (r->n_axes > 4 || r->rot_dim % 16 || r->rot_dim > D || r->pos_stride > kMaxStride)
         return QUAROT_ERR_UNSUPPORTED_SIZE;
-    if (r->positions ? r->pos_stride < T : !own_positions || r->n_axes != 1)
+    if (r->positions ? r->pos_stride < T : T > 0 && (!own_positions || r->n_axes != 1))
         return QUAROT_ERR_INVALID_ARG;
     if (!aligned4(r->positions) || !aligned4(r->inv_freq))
         return QUAROT_ERR_ALIGNMENT;

@@ -58,6 +58,10 @@ int main()
     };
     EXPECT(rope(rot), QUAROT_ERR_NO_DEVICE);
     EXPECT(rope(rot, 0), QUAROT_OK);
+    quarot_rotary none = rot;  // no tokens have no positions
+    none.positions = nullptr;
+    EXPECT(quarot_rope(nullptr, 512, nullptr, 512, &none, 0, 4, 128, 1, nullptr), QUAROT_OK);
+    EXPECT(rope(none), QUAROT_ERR_INVALID_ARG);
     EXPECT(quarot_rope(H, 512, O, 512, nullptr, 8, 4, 128, 1, nullptr), QUAROT_ERR_INVALID_ARG);
     EXPECT(quarot_rope(nullptr, 512, O, 512, &rot, 8, 4, 128, 1, nullptr), QUAROT_ERR_INVALID_ARG);
     for (int64_t bad : {M, int64_t(-1), BIG}) {

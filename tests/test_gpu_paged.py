@@ -587,3 +587,22 @@ def test_memory_of_a_call_on_another_stream(dev, orc, monkeypatch):
     assert len(on) == 4 and set(on) == {side.cuda_stream}
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want) and torch.equal(outs[1], turned)
+
+
+def test_no_tokens(dev):
+    """A batch without new tokens: nothing is done, and nothing refused."""
+    import torch
+    import paper_2404_00456_amd as q
+    bt = Batch(61, [0, 0], [40, 0], 2, 64, 32, 16)
+    args = [D_(a, dev) for a in (*bt.k, *bt.v, bt.table, bt.lens, bt.cu)]
+    before = [a.clone() for a in args]
+    x, kv = (torch.zeros(0, h, 64, dtype=torch.float16, device=dev) for h in (6, 2))
+    pos = torch.zeros(3, 0, dtype=torch.int32, device=dev)
+    fr = D_(freq(64), dev)
+    assert q.quarot_rope(x, pos[0], fr).shape == x.shape
+    assert q.quarot_rope(x, pos, fr, sections=[2, 15, 15], rotate=True).shape == x.shape
+    assert q.quarot_kv_append_paged(kv, kv, args[:3], args[3:6], *args[6:], group=32, q=x,
+                                    positions=pos, inv_freq=fr, sections=[2, 15, 15]).shape == x.shape
+    assert q.quarot_kv_paged_attention(x, args[:3], args[3:6], *args[6:], group=32).shape == x.shape
+    for a, b in zip(args, before):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
