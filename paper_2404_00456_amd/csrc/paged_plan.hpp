@@ -141,9 +141,13 @@ QUAROT_HD int64_t part_row(Which which, int64_t b, int64_t tok0, int64_t rep)
 // (64 of 1 .. 8192: 73 us in splits of 32 steps, 89 of 64), and few steps do best
 // in pieces of 4 (one of 4096: 10.5 us, 13 of 8, 21 of 24; but one of 32768: 22 of
 // 4, 19 of 8).  8192 blocks at most, which bounds the workspace as well.
+// Beside long sequences there are fewer than B of them (a mixed batch of 16: 291 us
+// for 512, 285 for 2048).
 inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
 {
-    const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * std::min<int64_t>(B * hkv, 1 << 20) / 512));
+    const int fill = which == FEW ? 2048 : 512;
+    const int64_t rows = std::min<int64_t>(B * hkv, 1 << 20);
+    const int least = (int)std::min<int64_t>(32, std::max<int64_t>(4, steps * rows / fill));
     const int64_t splits = std::min<int64_t>({(steps + least - 1) / least, 128, 8192 / (B * hkv)});
     return Part{which, FEW_ROWS, (int)std::max<int64_t>(1, splits), least};
 }
