@@ -218,7 +218,7 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
         n_heads > 0xFFFF || n_kv_heads <= 0 || n_heads % n_kv_heads || !head_dim_ok(head_dim) ||
         group <= 0 || max_seq_len <= 0 || window < 0 || n_sinks < 0)
         return 0;
-    const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim, group,
+    const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim,
                                    std::min(max_seq_len, kMaxTokens), std::min(window, kMaxTokens),
                                    std::min(n_sinks, kMaxTokens));
     return attention_workspace(p, T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim);
@@ -252,7 +252,7 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
     window = std::min(window, kMaxTokens);
     n_sinks = std::min(n_sinks, kMaxTokens);
     const int64_t hkv = cache->n_kv_heads, rep = n_heads / hkv;
-    const paged::Plan p = paged::plan(T, cache->batch, hkv, rep, D, cache->group,
+    const paged::Plan p = paged::plan(T, cache->batch, hkv, rep, D,
                                       std::min(max_seq_len, kMaxTokens), window, n_sinks);
     for (int i = 0; i < p.n; ++i)  // a launch holds fewer than 2^32 threads
         if (paged::slots(p.part[i], T, cache->batch, rep) * hkv * p.part[i].splits >

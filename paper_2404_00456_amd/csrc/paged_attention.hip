@@ -416,7 +416,7 @@ __global__ __launch_bounds__(64 * NW)
     constexpr int NT = 64 * NW, MR = 32 * NW;
     constexpr int KS = D / 16, DB = D / 32;
     // A stage holds 64 tokens, 32 for D = 256 and for two waves, of which then two
-    // blocks fit a CU (single tokens over 8192 in groups of 32: 197 us with 64).  While one's scores are taken and
+    // blocks fit a CU (16 sequences of one row over 8192: 142 us so, 197 with 64).  While one's scores are taken and
     // the last one's values are added, the next but one is written.
     constexpr int TS = D == 256 || NW == 2 ? 32 : 64, NB = TS == 32 ? 4 : 3;
     using St = Stage<D, TS>;
@@ -724,11 +724,11 @@ __global__ __launch_bounds__(64 * NW)
 // ---- few query rows: single tokens, and a few that were guessed ahead -------
 //
 // k_paged_rows: up to 16 query rows (new tokens times the heads of a cache head)
-// of a sequence, one group per cached row.  Four waves take the block's token
+// of a sequence, NG groups per cached row.  Four waves take the block's token
 // blocks of 64 in turn, straight from memory to registers, 16 tokens at a time
 // as in the dense decode kernels: A = the K codes as fp16 integers against B =
-// the queries, then A = the weights against B = the V codes.  Codes enter as
-// they are, so that nothing of a key or value is rounded:
+// the queries, then A = the weights against B = the V codes.  Where a row is one
+// group, codes enter as they are, so that nothing of a key or value is rounded:
 //   q . khat_t = ks_t (q . code_t) + kz_t sum(q),
 //   sum_t p_t vhat_t = sum_t (p_t vs_t) code_t + sum_t p_t vz_t.
 // A code c is or-ed into an fp16 significand: as 64 + c in the K operand, whose
@@ -745,6 +745,17 @@ __global__ __launch_bounds__(64 * NW)
 // 2^15.  (Scales below 2^-24, none but 0 in fp16, count as that, so that rows of
 // equal values have a reference.)
 //
+// Where a row is several groups, a key's constants belong to its elements and not to
+// its score: keys and values enter as RN16(code * scale + zero), the weights
+// rounded to fp16, as in the tiles, and m is the largest score's.  (16 sequences
+// over up to 8192 tokens, 32 heads on 8: 36 us with groups of 128, 39 of 64, 40 of
+// 32; by 64-row tiles 142.)
+//
+// What bounds it: a stage of 32 tokens is 4.3 KB for D = 128 and about 280 vector
+// instructions, 1100 cycles of a SIMD where the memory's share of one takes 2000;
+// but of the 17 us that a block of 1024 tokens takes 7 are its start (sequence,
+// pages, queries, first codes) and its end, which four blocks a CU hide only in
+// part.  64 sequences of 1 .. 8192 tokens: 69 us and 7 for their joining, 277 MB.
 // A wave's codes and constants come through a ring of its own in LDS, 32 tokens
 // a stage, by loads that go from memory straight there (16 bytes a lane): the
 // next stage is on its way while this one is multiplied, at no registers, and
@@ -752,11 +763,11 @@ __global__ __launch_bounds__(64 * NW)
 constexpr int ROWS_W = 4;   // waves of a block
 constexpr int ROWS_NS = 2;  // stages of a wave's ring
 
-template <int D>
+template <int D, int NG>
 struct RowsRing {
     static constexpr int KB = 32 * D / 2;  // bytes of a stage's K codes, and of its V codes
-    static constexpr int STAGE = 2 * KB + 256;  // and ks, kz, vs, vz of 32 tokens
-    static constexpr int LOADS = 2 * (KB / 1024) + 1;
+    static constexpr int STAGE = 2 * KB + 256 * NG;  // and ks, kz, vs, vz of 32 tokens
+    static constexpr int LOADS = 2 * (KB / 1024) + NG;
     static constexpr int UPR = D / 32;  // 16-byte units of a row
     // K: unit c of row n at c ^ swz(n), so that 16 rows' same unit falls on
     // different banks
@@ -772,11 +783,12 @@ struct RowsRing {
     }
 };
 
-template <int D>
+template <int D, int NG>
 __global__ __launch_bounds__(64 * ROWS_W)
     __attribute__((amdgpu_waves_per_eu(D == 256 ? 2 : 4, D == 256 ? 2 : 4))) void k_paged_rows(PagedAttnArgs a)
 {
-    using Ring = RowsRing<D>;
+    using Ring = RowsRing<D, NG>;
+    constexpr int G = D / NG;
     constexpr int MR = paged::FEW_ROWS;
     constexpr int KW = D / 32;  // dwords of K codes of a lane: D / 4 elements of a token
     constexpr int VD = D / 16;  // dimensions of a lane in the value product
@@ -826,8 +838,15 @@ __global__ __launch_bounds__(64 * ROWS_W)
         koff[x] = rw * (D / 2) + (c ^ Ring::swz(rw)) * 16;
         voff[x] = Ring::token_of(rw) * (D / 2) + c * 16;
     }
-    const uint16_t *carr = lane < 16 ? a.kp.s : lane < 32 ? a.kp.z : lane < 48 ? a.vp.s : a.vp.z;
-    carr += (lane & 7) * 2;
+    // constants: [array][16-token group][token][group of the row], 256 bytes a load
+    const uint16_t *carr[NG];
+    int cgrp[NG];
+#pragma unroll
+    for (int x = 0; x < NG; ++x) {
+        const int b = 256 * x + 4 * lane, arr = b / (64 * NG), rem = b % (64 * NG);
+        cgrp[x] = rem / (32 * NG);
+        carr[x] = (arr < 2 ? arr ? a.kp.z : a.kp.s : arr < 3 ? a.vp.s : a.vp.z) + rem % (32 * NG) / 2;
+    }
 
     int64_t base = -1;  // pool rows of the next 64 groups of 16 tokens, one a lane
     auto look = [&](int k) {
@@ -871,7 +890,9 @@ __global__ __launch_bounds__(64 * ROWS_W)
                            at + Ring::KB + (u * (16 / TPL) + x) * 1024);
                 }
         }
-        dma4(carr + (lane & 8 ? r0[1] : r0[0]), at + 2 * Ring::KB);
+#pragma unroll
+        for (int x = 0; x < NG; ++x)
+            dma4(carr[x] + (cgrp[x] ? r0[1] : r0[0]) * NG, at + 2 * Ring::KB + 256 * x);
         return ok;
     };
 
@@ -909,7 +930,12 @@ __global__ __launch_bounds__(64 * ROWS_W)
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
         const uint8_t *stg = ring + (k % ROWS_NS) * Ring::STAGE;
-        const uint8_t *cst = stg + 2 * Ring::KB + 8 * g;  // + 64 array + 32 group
+        // one group a row: constants of tokens 4 g + r, + 64 array + 32 group
+        const uint8_t *cst = stg + 2 * Ring::KB + 8 * g;
+        auto constant = [&](int arr, int u, int token, int grp) {
+            return (uint32_t)*reinterpret_cast<const uint16_t *>(
+                stg + 2 * Ring::KB + (64 * NG * arr + 32 * NG * u) + (token * NG + grp) * 2);
+        };
         float x[2][4];
         _Float16 ksh[2][4], kzh[2][4], vsh[2][4], vzh[2][4];  // enter v_fma_mix as they are
         auto halfs = [&](int arr, int u, _Float16 *f) {
@@ -936,6 +962,32 @@ __global__ __launch_bounds__(64 * ROWS_W)
                                              kr + (((KW / 4) * g + c) ^ Ring::swz(n)) * 16, 16), 16);
                 }
             }
+            if constexpr (NG > 1) {
+                // this lane's piece of token n lies in one group, or in two halves in two
+                constexpr int PG = NG > 4 ? NG / 4 : 1;
+                v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int p = 0; p < PG; ++p) {
+                    const int grp = (D / 4 * g + 8 * (p * (KW / PG))) / G;
+                    const uint32_t ks = constant(0, u, n, grp), kz = constant(1, u, n, grp);
+                    const h2v s = bits_h2(ks | ks << 16), z = bits_h2(kz | kz << 16);
+#pragma unroll
+                    for (int c = p * (KW / PG); c < (p + 1) * (KW / PG); ++c) {
+                        auto two = [&](uint32_t w, bool hi) {
+                            return __builtin_bit_cast(
+                                uint32_t, fma2(hi ? nib_pair<true>(w, nk) : nib_pair<false>(w, nk), s, z));
+                        };
+                        const uint4 kf = make_uint4(two(kc[c], false), two(kc[c], true),
+                                                    two(kc[c] >> 8, false), two(kc[c] >> 8, true));
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, kf), qb[c],
+                                                                     acc, 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[u][r] = __builtin_fmaf(acc[r], c2, -ms);
+                continue;
+            }
             v4f acc = {q64, q64, q64, q64};
 #pragma unroll
             for (int c = 0; c < KW; ++c) {
@@ -954,7 +1006,8 @@ __global__ __launch_bounds__(64 * ROWS_W)
                 x[u][r] = __builtin_fmaf((float)ksh[u][r], acc[r] * c2,
                                          __builtin_fmaf((float)kzh[u][r], qs, -ms));
         }
-        if (ok != 3 || th + 31 > pmin || (a.window > 0 && th <= pmax - a.window)) {
+        const bool edge = ok != 3 || th + 31 > pmin || (a.window > 0 && th <= pmax - a.window);
+        if (edge) {
             asm volatile("");  // a branch, not selects in every step
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -963,6 +1016,8 @@ __global__ __launch_bounds__(64 * ROWS_W)
                     const int t = th + 16 * u + 4 * g + r;
                     const bool see = (ok >> u & 1) && t <= p && (t > wfirst || t < a.sinks);
                     x[u][r] = see ? x[u][r] : -inf;
+                    if constexpr (NG > 1)
+                        continue;
                     // a weight of 0 times what a slot that was never written
                     // holds may be NaN
                     vsh[u][r] = see ? vsh[u][r] : (_Float16)0.0f;
@@ -978,8 +1033,9 @@ __global__ __launch_bounds__(64 * ROWS_W)
                 for (int r = 0; r < 4; ++r) {
                     const float e = __builtin_amdgcn_exp2f(x[u][r]);
                     ln += e;
-                    zn = __builtin_fmaf(e, (float)vzh[u][r], zn);
-                    wt[u][r] = __builtin_fmaf(e, (float)vsh[u][r], 0.0f);
+                    if constexpr (NG == 1)
+                        zn = __builtin_fmaf(e, (float)vzh[u][r], zn);
+                    wt[u][r] = NG == 1 ? __builtin_fmaf(e, (float)vsh[u][r], 0.0f) : e;
                     most = fmaxf(most, wt[u][r]);
                 }
         };
@@ -991,7 +1047,9 @@ __global__ __launch_bounds__(64 * ROWS_W)
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    y = fmaxf(y, x[u][r] + __builtin_amdgcn_logf(fmaxf((float)vsh[u][r], 0x1p-24f)));
+                    y = fmaxf(y, NG > 1 ? x[u][r]
+                                        : x[u][r] + __builtin_amdgcn_logf(
+                                                        fmaxf((float)vsh[u][r], 0x1p-24f)));
             y = lane_max<4>(y);
             y = lane_max<5>(y);
             const float mn = fmaxf(m, ms + y);
@@ -1023,6 +1081,11 @@ __global__ __launch_bounds__(64 * ROWS_W)
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
+                if constexpr (NG > 1) {
+                    const h2v w2 = {(_Float16)wt[u][r], (_Float16)wt[u][r + 1]};
+                    hh[2 * u + r / 2] = __builtin_bit_cast(uint32_t, w2);
+                    continue;
+                }
                 // the first part truncated, the second what that leaves
                 const h2v hi = pk_rtz(wt[u][r], wt[u][r + 1]);
                 hh[2 * u + r / 2] = __builtin_bit_cast(uint32_t, hi);
@@ -1031,7 +1094,26 @@ __global__ __launch_bounds__(64 * ROWS_W)
                                      __builtin_fmaf((float)hi[1], -1.0f, wt[u][r + 1])));
             }
         const v8h wh = __builtin_bit_cast(v8h, make_uint4(hh[0], hh[1], hh[2], hh[3]));
-        const v8h wl = __builtin_bit_cast(v8h, make_uint4(ll[0], ll[1], ll[2], ll[3]));
+        const v8h wl = NG > 1 ? v8h{} : __builtin_bit_cast(v8h, make_uint4(ll[0], ll[1], ll[2], ll[3]));
+        // constants of the values' pairs of tokens, in this lane's dimensions' group
+        h2v vs2[4], vz2[4];
+        if constexpr (NG > 1) {
+            const int grp = VD * n / G;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int u = x >> 1, t = 4 * g + 2 * (x & 1);
+                uint32_t keep = 0xFFFFFFFFu;
+                if (edge) {  // tokens that no row sees
+                    auto held = [&](int tt) {
+                        return (ok >> u & 1) && tt < w.hi && (tt >= w.low || tt < a.sinks);
+                    };
+                    keep = (held(th + 16 * u + t) ? 0xFFFFu : 0u) |
+                           (held(th + 16 * u + t + 1) ? 0xFFFF0000u : 0u);
+                }
+                vs2[x] = bits_h2((constant(2, u, t, grp) | constant(2, u, t + 1, grp) << 16) & keep);
+                vz2[x] = bits_h2((constant(3, u, t, grp) | constant(3, u, t + 1, grp) << 16) & keep);
+            }
+        }
         uint32_t vc[2][4][(VD + 7) / 8];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -1058,15 +1140,21 @@ __global__ __launch_bounds__(64 * ROWS_W)
                     const uint32_t b2 = perm_b32(vc[u][2 * t + 1][wd], vc[u][2 * t][wd], sel);
                     lo[2 * u + t] = nib_pair<false>(b2, nk);
                     hi[2 * u + t] = nib_pair<true>(b2, nk);
+                    if constexpr (NG > 1) {
+                        lo[2 * u + t] = fma2(lo[2 * u + t], vs2[2 * u + t], vz2[2 * u + t]);
+                        hi[2 * u + t] = fma2(hi[2 * u + t], vs2[2 * u + t], vz2[2 * u + t]);
+                    }
                 }
             const v8h vlo = {lo[0][0], lo[0][1], lo[1][0], lo[1][1],
                              lo[2][0], lo[2][1], lo[3][0], lo[3][1]};
             const v8h vhi = {hi[0][0], hi[0][1], hi[1][0], hi[1][1],
                              hi[2][0], hi[2][1], hi[3][0], hi[3][1]};
             o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, vlo, o[2 * bt], 0, 0, 0);
-            o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vlo, o[2 * bt], 0, 0, 0);
+            if constexpr (NG == 1)
+                o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vlo, o[2 * bt], 0, 0, 0);
             o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, vhi, o[2 * bt + 1], 0, 0, 0);
-            o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
+            if constexpr (NG == 1)
+                o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
         }
     }
 
@@ -1225,7 +1313,19 @@ hipError_t go_few(const PagedAttnArgs &a, hipStream_t s)
     constexpr int MR = paged::FEW_ROWS;
     const int slots = (int)paged::slots({a.which, MR}, a.map.T, a.map.B, a.rep);
     const dim3 grid((unsigned)((int64_t)slots * a.hkv * a.splits));
-    hipLaunchKernelGGL((k_paged_rows<D>), grid, dim3(64 * ROWS_W), 0, s, a);
+    const dim3 block(64 * ROWS_W);
+    switch (D / a.G) {
+    case 1: hipLaunchKernelGGL((k_paged_rows<D, 1>), grid, block, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((k_paged_rows<D, 2>), grid, block, 0, s, a); break;
+    case 4:
+        if constexpr (D >= 128)
+            hipLaunchKernelGGL((k_paged_rows<D, 4>), grid, block, 0, s, a);
+        break;
+    case 8:
+        if constexpr (D >= 256)
+            hipLaunchKernelGGL((k_paged_rows<D, 8>), grid, block, 0, s, a);
+        break;
+    }
     hipError_t e = hipGetLastError();
     return e != hipSuccess || a.splits == 1 ? e : go_combine<D, MR>(a, slots, s);
 }

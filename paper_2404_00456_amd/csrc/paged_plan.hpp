@@ -155,8 +155,8 @@ inline Part few_part(Which which, int64_t steps, int64_t B, int64_t hkv)
 // Tiles: 256 blocks, one a CU as LDS holds them (two of the 64-row tile): a second
 // turn of blocks costs more than the joining of fewer splits saves (512 new tokens
 // over 16384, 64 heads on 8: 319 us in 256 blocks, 329 in 512; 4 x 64 over 8192: 70
-// and 101; single tokens over 8192 in groups of 32, 64-row tiles: 142 us in 512
-// blocks, 223 in 256).
+// and 101; 64-row tiles that 16 sequences of one row fill: 142 us in 512 blocks, 223
+// in 256).
 inline Part tile_part(Which which, int64_t steps, int64_t rows, int64_t T, int64_t B, int64_t hkv,
                       int64_t rep, int64_t D)
 {
@@ -172,7 +172,7 @@ inline Part tile_part(Which which, int64_t steps, int64_t rows, int64_t T, int64
 // T new tokens of B sequences, hkv cache heads with rep query heads each, at
 // most max_len cached tokens.  Only a rule of speed: any content of cu and len
 // is right under any plan.
-inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int64_t G,
+inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D,
                  int64_t max_len, int64_t window, int64_t sinks)
 {
     // query rows of a sequence: on average, and of the longest at most (where
@@ -180,7 +180,7 @@ inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D, int6
     const int64_t rows = (T * rep + B - 1) / B, most = std::max<int64_t>(T - B + 1, 1) * rep;
     const int64_t seen = window > 0 ? std::min(max_len, window + sinks + T / B) : max_len;
     const int64_t steps = (seen + STEP - 1) / STEP;
-    if (G != D || rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
+    if (rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
         return Plan{1, {tile_part(ALL, steps, rows, T, B, hkv, rep, D)}};
     // Sequences of few rows: guessed tokens of 64 sequences, 16 rows each, take 66 us
     // so and 84 with a launch for longer ones beside; but a batch of single tokens

@@ -136,7 +136,7 @@ static void plans()
                     for (int64_t D : {64, 128, 256})
                         for (int64_t len : {1, 64, 300, 4096, 32768, 1 << 30})
                             for (int64_t window : {0, 1, 1000, 1 << 30}) {
-                                const Plan p = plan(T, B, hkv, rep, D, T % 3 ? D : 32, len, window,
+                                const Plan p = plan(T, B, hkv, rep, D, len, window,
                                                     1 << 30);
                                 CHECK(p.n == 1 || p.n == 2, "launches");
                                 // every sequence in one launch
@@ -148,7 +148,6 @@ static void plans()
                                     CHECK(t.least >= 1 && (int64_t)t.least * t.splits < 1 << 20, "least");
                                     CHECK(t.splits >= 1 && t.splits <= 128, "splits %d", t.splits);
                                     CHECK(t.rows == 16 || t.rows == 64 || t.rows == 128 || t.rows == 256, "rows");
-                                    CHECK(t.rows != 16 || T % 3 || D == 32, "whole groups");
                                     CHECK(t.which != FEW || t.rows == FEW_ROWS, "few");
                                     // partial rows of every block fit
                                     CHECK(t.splits == 1 || part_row(t.which, B - 1, T - 1, rep) <

@@ -285,6 +285,23 @@ def test_mixed_batches(dev, orc, D, G, H, hkv, page, new):
         check(dev, orc, bt, H, max_seq_len=30000)
 
 
+@pytest.mark.parametrize("D,G", [(64, 32), (128, 32), (128, 64), (256, 32), (256, 64), (256, 128)])
+@pytest.mark.parametrize("exact", [True, False])
+@pytest.mark.parametrize("new,total,page", [([1, 1, 1, 1], [1, 33, 700, 128], 16),
+                                            ([2, 1, 0, 4], [65, 1, 9, 515], 48),
+                                            ([1] * 9 + [9], [40 * i + 1 for i in range(9)] + [333], 64)])
+def test_few_rows_in_groups(dev, orc, D, G, exact, new, total, page):
+    """Few rows whose cached rows are several groups, with and without a window,
+    whole and in splits."""
+    bt = Batch(70 + D, new, total, 2, D, G, page, behind=1, exact=exact)
+    check(dev, orc, bt, 8, exact=exact)
+    check(dev, orc, bt, 2, window=70, sinks=3, exact=exact)
+    check(dev, orc, bt, 8, max_seq_len=1 << 16, exact=exact)
+    for pool in (bt.k, bt.v):  # groups of equal values
+        pool[1][..., ::2][np.broadcast_to(bt.held[:, None, :, None], pool[1][..., ::2].shape)] = 0
+    check(dev, orc, bt, 8, exact=exact)
+
+
 def test_large_scores(dev, orc):
     """Queries whose scores reach hundreds: one token takes all the weight."""
     check(dev, orc, Batch(9, [1, 40], [300, 300], 2, 128, 128, 16), 8, sigma=60.0)
