@@ -302,6 +302,31 @@ def test_few_rows_in_groups(dev, orc, D, G, exact, new, total, page):
     check(dev, orc, bt, 8, exact=exact)
 
 
+@pytest.mark.parametrize("D,G", [(128, 128), (64, 32)])
+@pytest.mark.parametrize("new,first", [([1, 1, 40], 2), ([20, 1, 1], 33), ([1, 1, 1, 1], 100),
+                                       ([300], 19)])
+def test_rows_before_the_first_sequence(dev, orc, D, G, new, first):
+    """cu_new need not begin at 0: rows in front belong to nobody as well."""
+    import torch
+    import paper_2404_00456_amd as q
+    bt = Batch(90, new, [n + 70 for n in new], 2, D, G, 16, behind=first + 1)
+    bt.cu += first
+    check(dev, orc, bt, 4)
+    check(dev, orc, bt, 16, max_seq_len=1 << 15)
+    k, v = (torch.randn(bt.T, 2, D, device=dev).half() for _ in range(2))
+    x = torch.randn(bt.T, 4, D, device=dev).half()
+    pools = [tuple(D_(a, dev) for a in p) for p in (bt.k, bt.v)]
+    out = torch.full_like(x, 9.0)
+    q.quarot_kv_append_paged(k, v, *pools, D_(bt.table, dev), D_(bt.lens, dev), D_(bt.cu, dev),
+                             group=G, q=x, q_out=out)
+    assert (out[:first] == 9.0).all() and (out[bt.cu[-1]:] == 9.0).all()
+    for pool, host, rows in ((pools[0], bt.k, orc.rotate_rows(k.cpu().numpy().astype(np.float32))),
+                             (pools[1], bt.v, v.cpu().numpy().astype(np.float32))):
+        ref = orc.kv_append_paged(rows, host, bt.table, bt.lens, bt.cu, G)
+        for a, b in zip(pool, ref):
+            assert np.array_equal(a.cpu().numpy().view(np.uint8), b.view(np.uint8))
+
+
 def test_large_scores(dev, orc):
     """Queries whose scores reach hundreds: one token takes all the weight."""
     check(dev, orc, Batch(9, [1, 40], [300, 300], 2, 128, 128, 16), 8, sigma=60.0)
