@@ -1288,7 +1288,9 @@ hipError_t go_combine(const PagedAttnArgs &a, int slots, hipStream_t s)
         hipLaunchKernelGGL((k_paged_combine<D, MR, 4>), dim3(x, (unsigned)std::min(MR, a.rep * 4)),
                            dim3(256), 0, s, a);
     else
-        hipLaunchKernelGGL((k_paged_combine<D, MR, 1>), dim3(x, (unsigned)std::max(1, MR / 32)),
+        // rows of a block row are shared by blocks of eight (16 in one block: 8
+        // sequences of 4096 19 us instead of 18)
+        hipLaunchKernelGGL((k_paged_combine<D, MR, 1>), dim3(x, MR == paged::FEW_ROWS ? 2 : MR / 32),
                            dim3(256), 0, s, a);
     return hipGetLastError();
 }
