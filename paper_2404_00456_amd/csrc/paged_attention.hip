@@ -154,6 +154,16 @@ __device__ __forceinline__ h2v fma2(h2v a, h2v b, h2v c)
     return __builtin_elementwise_fma(a, b, c);
 }
 
+// Two scale and zero pairs: bit 15 of the half of those under which some code would
+// not be a finite fp16 value (code * s + z lies between z and 15 s + z, and so does
+// its rounding; an exponent of all ones carries there).
+__device__ __forceinline__ uint32_t spoils(uint32_t s, uint32_t z)
+{
+    const h2v fifteen = {(_Float16)15.0f, (_Float16)15.0f};
+    const uint32_t b = __builtin_bit_cast(uint32_t, fma2(bits_h2(s), fifteen, bits_h2(z)));
+    return ((b & 0x7FFF7FFFu) + 0x04000400u) & 0x80008000u;
+}
+
 // 16 bytes of 8 fp16 elements in the order 0, 4, 1, 5, 2, 6, 3, 7, in which
 // the nibble pairs of a dword of codes come out
 __device__ __forceinline__ uint4 nib_order(uint4 r)
@@ -213,6 +223,8 @@ struct Ahead {
     const PagedAttnArgs &a;
     const Work &w;
     int h, wave, lane;
+    int pmin, after;                 // every row sees the tokens behind after, up to pmin
+    int *spoiled;                    // this wave's, in LDS
     int64_t krow[S::N], vrow[S::N];  // pool rows of the groups of the next read, or -1
     int vt[S::N];                    // first token of the values' group
     uint32_t kc[S::N][S::EK / 8];    // codes
@@ -328,10 +340,12 @@ struct Ahead {
                 vs[i] = make_uint2(s[0] | (s[1] << 16), s[2] | (s[3] << 16));
                 vz[i] = make_uint2(z[0] | (z[1] << 16), z[2] | (z[3] << 16));
             }
-            // tokens that no row sees take a weight of 0, and 0 times what a slot
-            // holds that was never written may be NaN
+            // Tokens that a row does not see take a weight of 0 in it, and 0 times what
+            // is not finite would be NaN: those that no row sees (slots that were never
+            // written) are taken as 0, and so are those of the others that are not
+            // finite, which the rows that see them take at the end (add_spoiled).
             const int g0 = __builtin_amdgcn_readfirstlane(vt[i]);
-            if (__builtin_expect(!(in & (g0 + 16 <= w.hi) & (g0 >= w.low)), 0)) {
+            if (__builtin_expect(!(in & (g0 + 15 <= pmin) & (g0 > after)), 0)) {
                 uint32_t keep[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -341,6 +355,13 @@ struct Ahead {
                 const uint32_t k01 = keep[0] | (keep[1] << 16), k23 = keep[2] | (keep[3] << 16);
                 vs[i] = make_uint2(vs[i].x & k01, vs[i].y & k23);
                 vz[i] = make_uint2(vz[i].x & k01, vz[i].y & k23);
+                const uint32_t b01 = spoils(vs[i].x, vz[i].x), b23 = spoils(vs[i].y, vz[i].y);
+                if (b01 | b23) {
+                    const uint32_t m01 = ~((b01 >> 15) * 0xFFFFu), m23 = ~((b23 >> 15) * 0xFFFFu);
+                    vs[i] = make_uint2(vs[i].x & m01, vs[i].y & m23);
+                    vz[i] = make_uint2(vz[i].x & m01, vz[i].y & m23);
+                    *spoiled = 1;
+                }
             }
         }
     }
@@ -408,6 +429,170 @@ __device__ __forceinline__ Place place(const PagedAttnArgs &a)
     return p;
 }
 
+// The arguments (a kernel's first) once more, for code that hardly ever runs: their
+// fields would otherwise be kept for it in scalar registers through the main loop.
+__device__ __forceinline__ PagedAttnArgs args_again()
+{
+    auto p = (const __attribute__((address_space(4))) PagedAttnArgs *)(
+        __builtin_amdgcn_kernarg_segment_ptr());
+    asm volatile("" : "+s"(p));
+    return *(const PagedAttnArgs *)p;
+}
+
+// One row of a block by one wave, token by token, a token seen or not touched at
+// all: for blocks of few rows in several groups that hold a value that is not finite
+// and that only some of the rows see, since the products of all rows with all tokens
+// would make 0 times it of the others.  (64 sequences of 4 new tokens: 71 us, 2.5 ms
+// so.)  64 scores at a time, a token a lane; then each seen token's value, D /
+// 64 elements a lane.  The result goes where the block's goes.
+template <int D>
+__device__ __forceinline__ void row_alone(const PagedAttnArgs &a, const Work &w, const Place &pl, int row)
+{
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63, ng = D / a.G;
+    const int qi = row / a.rep, p = w.pos0 + qi, head = pl.h * a.rep + (row - qi * a.rep);
+    const int64_t trow = w.tok0 + qi;
+    const uint16_t *q = a.q + trow * a.q_stride + (int64_t)head * D;
+    const int first = a.window > 0 ? p - a.window : -1;
+    const float inf = __builtin_inff(), c2 = a.sm_scale * 1.44269504088896340736f;
+    float m = -inf, l = 0.0f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        o[e] = 0.0f;
+    const int begin = pl.split * w.per, end = min(w.steps, begin + w.per);
+#pragma unroll 1
+    for (int i = begin; i < end; ++i) {
+        const int t = paged::step_token(w, i) + lane;
+        int64_t at = pool_row(a.map, a.hkv, w.b, t);
+        const bool see = at >= 0 && t <= p && (t > first || t < a.sinks);
+        const uint64_t seen = __ballot(see);
+        if (seen == 0)
+            continue;
+        at = see ? at + (int64_t)pl.h * a.map.page : 0;
+        float x = 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < D / 8; ++k) {
+            const uint32_t c = *reinterpret_cast<const uint32_t *>(a.kp.c + at * (D / 2) + 4 * k);
+            const int64_t gi = at * ng + 8 * k / a.G;
+            const float s = h2f(a.kp.s[gi]), z = h2f(a.kp.z[gi]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x = __builtin_fmaf(h2f(q[8 * k + e]),
+                                   __builtin_fmaf((float)((c >> (4 * e)) & 15u), s, z), x);
+        }
+        x = see ? x * c2 : -inf;
+        float mn = x;
+        static_for<6>([&](auto J) { mn = lane_max<J>(mn); });
+        mn = fmaxf(m, mn);
+        const float ms = mn > -inf ? mn : 0.0f;
+        const float f = m > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.0f;
+        const float wt = see ? __builtin_amdgcn_exp2f(x - ms) : 0.0f;
+        m = mn;
+        l = l * f + wt;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            o[e] *= f;
+#pragma unroll 1
+        for (int j0 = 0; j0 < 64; j0 += 8)
+#pragma unroll
+            for (int j = j0; j < j0 + 8; ++j) {
+                const int64_t aj = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), j) << 32) |
+                                             (uint32_t)__builtin_amdgcn_readlane((int)at, j));
+                const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), j));
+                const uint8_t *c = a.vp.c + aj * (D / 2) + lane * E / 2;
+                const int64_t gi = aj * ng + lane * E / a.G;
+                const float s = h2f(a.vp.s[gi]), z = h2f(a.vp.z[gi]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int sh = E == 1 ? (lane & 1) * 4 : (e & 1) * 4;
+                    const float v = __builtin_fmaf((float)((c[e / 2] >> sh) & 15), s, z);
+                    o[e] = __builtin_fmaf(wj, seen >> j & 1 ? v : 0.0f, o[e]);
+                }
+            }
+    }
+    for (int d = 1; d < 64; d <<= 1)
+        l += __shfl_xor(l, d);
+    if (w.used == 1) {
+        const float f = l > 0.0f ? 1.0f / l : 0.0f;
+        uint16_t *dst = a.out + trow * a.out_stride + (int64_t)head * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            dst[e] = f2h(o[e] * f);
+    } else {
+        const int64_t pr = part_of(a, w, row, pl.h) + pl.split;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            a.part_o[pr * D + lane * E + e] = o[e];
+        if (lane == 0)
+            *reinterpret_cast<float2 *>(a.part_ml + 2 * pr) = make_float2(m, l);
+    }
+}
+
+// What a row of a tile takes from the values of group g0 that are not finite, this
+// lane's half of its dimensions.  m is its final reference; its sum has these tokens'
+// weights already.  (A prompt of 8192 takes 1.2 ms, with such a value in its last
+// token as much, with nothing else in its cache 2.4 ms.  The look at each group that
+// some rows see and some do not costs short prompts and windows 1 to 2%.)
+template <int D>
+__device__ __forceinline__ void add_spoiled(const PagedAttnArgs &a, const Work &w, int h, int g0, int p,
+                                            const uint16_t *q, float m, v16f *o)
+{
+    const int lane = threadIdx.x & 63, hf = lane >> 5, ng = D / a.G;
+    int64_t row = pool_row(a.map, a.hkv, w.b, g0);
+    if (row < 0)
+        return;
+    row += (int64_t)h * a.map.page;
+    bool odd = false;
+    const int tl = g0 + (lane & 15);
+    if (tl < w.hi && (tl >= w.low || tl < a.sinks))
+        for (int x = 0; x < ng; ++x) {
+            const int64_t gi = (row + (lane & 15)) * ng + x;
+            odd |= (spoils(a.vp.s[gi], a.vp.z[gi]) & 0x8000u) != 0;
+        }
+    const NibConst nk = nib_const();
+    for (uint32_t left = (uint32_t)__ballot(odd) & 0xFFFFu; left; left &= left - 1) {
+        const int t = g0 + __builtin_ctz(left);
+        const int64_t r1 = row + (t - g0);
+        float x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {  // as the matrix product has them
+            const int e = 16 * k + 8 * hf;
+            const v8h qv = __builtin_bit_cast(v8h, nib_order(*reinterpret_cast<const uint4 *>(q + e)));
+            const uint32_t c = *reinterpret_cast<const uint32_t *>(a.kp.c + r1 * (D / 2) + e / 2);
+            const uint32_t s1 = a.kp.s[r1 * ng + e / a.G], z1 = a.kp.z[r1 * ng + e / a.G];
+            const h2v s = bits_h2(s1 | s1 << 16), z = bits_h2(z1 | z1 << 16);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const uint32_t cy = y & 2 ? c >> 8 : c;
+                const h2v kv = fma2(y & 1 ? nib_pair<true>(cy, nk) : nib_pair<false>(cy, nk), s, z);
+                x = __builtin_fmaf((float)kv[0], (float)qv[2 * y], x);
+                x = __builtin_fmaf((float)kv[1], (float)qv[2 * y + 1], x);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (all loads at once take registers that D = 256 lacks)
+        }
+        const auto sw =
+            __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = (__uint_as_float(sw[0]) + __uint_as_float(sw[1])) * (a.sm_scale * 1.44269504088896340736f);
+        const bool see = t <= p && (a.window == 0 || t > p - a.window || t < a.sinks);
+        const float wt = __builtin_amdgcn_exp2f(x - (m > -__builtin_inff() ? m : 0.0f));
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int e = 32 * d + 2 * r + 4 * hf;
+                const uint32_t c = *reinterpret_cast<const uint16_t *>(a.vp.c + r1 * (D / 2) + e / 2);
+                const uint16_t s1 = a.vp.s[r1 * ng + e / a.G], z1 = a.vp.z[r1 * ng + e / a.G];
+                const bool take = see && (spoils(s1, z1) & 0x8000u) != 0;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float v = __builtin_fmaf((float)((c >> (4 * y)) & 15u), h2f(s1), h2f(z1));
+                    o[d][r + y] = __builtin_fmaf(take ? wt : 0.0f, take ? v : 0.0f, o[d][r + y]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+}
+
 // 32 query rows for each of NW waves.
 template <int D, int NW, bool ONE>
 __global__ __launch_bounds__(64 * NW)
@@ -422,6 +607,7 @@ __global__ __launch_bounds__(64 * NW)
     using St = Stage<D, TS>;
     using Sh = Share<D, TS, NT>;
     __shared__ __align__(16) St st[NB];
+    __shared__ int spoiled[NW];  // by wave: it left out values that are not finite
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, hf = lane >> 5;
     Place pl = place(a);
@@ -559,7 +745,9 @@ __global__ __launch_bounds__(64 * NW)
             const int k = min(j, (end - begin) * H - 1);
             return paged::step_token(w, begin + k / H) + k % H * TS;
         };
-        Ahead<D, TS, NT, ONE> ah{a, w, pl.h, __builtin_amdgcn_readfirstlane(wave), lane};
+        spoiled[wave] = 0;
+        Ahead<D, TS, NT, ONE> ah{a, w, pl.h, __builtin_amdgcn_readfirstlane(wave), lane,
+                                 pmin, a.window > 0 ? pmax - a.window : -1, spoiled + wave};
         auto put_all = [&](auto &from, St &to) {
 #pragma unroll
             for (int x = 0; x < Sh::PAIRS; ++x) {
@@ -687,6 +875,19 @@ __global__ __launch_bounds__(64 * NW)
                         st[last].v + St::vrow(32 * (c % DB) + n) +
                         St::vunit(32 * (c % DB) + n, c / DB * 2 + hf)),
                     pb[c / DB], o[c % DB], 0, 0, 0);
+        }
+        // values that read_values left out (the last stage's were read before the last
+        // barrier)
+        int any = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+            any |= spoiled[i];
+        if (__builtin_expect(any != 0, 0)) {
+            const PagedAttnArgs again = args_again();
+            for (int i = begin; i < end; ++i)
+                for (int g0 = paged::step_token(w, i), g1 = g0 + 64; g0 < g1; g0 += 16)
+                    if (!(g0 + 15 <= ah.pmin && g0 > ah.after))
+                        add_spoiled<D>(again, w, pl.h, g0, p, qr, m, o);
         }
     }
 
@@ -1155,6 +1356,32 @@ __global__ __launch_bounds__(64 * ROWS_W)
             o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, vhi, o[2 * bt + 1], 0, 0, 0);
             if constexpr (NG == 1)
                 o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, vhi, o[2 * bt + 1], 0, 0, 0);
+        }
+    }
+
+    if constexpr (NG > 1) {
+        // Values that only some rows see have to be finite (weights of one group's rows
+        // are masked row by row instead).  All waves look at all of them: no more than
+        // 15 behind the first row's position, and as many where windows begin.  (Looked
+        // at where they pass through, single tokens, which have none, took 41 us
+        // instead of 39.)
+        if (pmin != pmax) {
+            const PagedAttnArgs again = args_again();
+            const int behind = pmax - pmin, of = (again.window > 0 ? 2 : 1) * behind * NG;
+            bool odd = false;
+            for (int i = lane; i < of; i += 64) {
+                const int j = i / NG;
+                const int t = j < behind ? pmin + 1 + j : pmax - again.window - (j - behind);
+                const int64_t at = pool_row(again.map, again.hkv, w.b, t);
+                const int64_t gi = (at + (int64_t)pl.h * again.map.page) * NG + i % NG;
+                if (at >= 0 && t < w.hi)
+                    odd |= (spoils(again.vp.s[gi], again.vp.z[gi]) & 0x8000u) != 0;
+            }
+            if (__any(odd)) {
+                for (int r = wave; r < R; r += ROWS_W)
+                    row_alone<D>(again, w, pl, w.row0 + r);
+                return;
+            }
         }
     }
 
