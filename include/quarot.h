@@ -626,12 +626,14 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
  * at position p sees the cached tokens t <= p with
  *   window == 0  or  t > p - window  or  t < n_sinks,
  * and out = RN16(softmax_t(sm_scale * q . khat_t) . vhat), khat and vhat the
- * dequantized rows (rounded to fp16 where a kernel multiplies them as such),
- * weights rounded to fp16 for their product, sums and softmax in binary32; a
- * query that sees nothing gives zeros.  What a query does not see (later tokens,
- * slots past a sequence, pages before its window) has no influence on its
- * output, whatever the scales hold; a value that is not finite makes the
- * elements of its group not finite for the queries that see it.
+ * dequantized rows, sums and softmax in binary32.  At most 16 query rows a
+ * sequence (new tokens times query heads of a cache head; where batch is 1, T
+ * counts) with one group a row take codes as they are and weights in two fp16
+ * parts; other calls may round khat, vhat and the weights to fp16 for their
+ * products.  A query that sees nothing gives zeros.  What a query does not see
+ * (later tokens, slots past a sequence, pages before its window) has no
+ * influence on its output, whatever the scales hold; a value that is not finite
+ * makes the elements of its group not finite for the queries that see it.
  *   q fp16, head h of token t at q + t * q_stride + h * head_dim; query head h
  *   reads cache head h / (n_heads / n_kv_heads); out alike with out_stride,
  *   not overlapping q.  Rows of no sequence are not written.

@@ -939,12 +939,17 @@ __global__ __launch_bounds__(64 * NW)
 // is small beside the sum of its weights, and offsets of 128 left in the
 // products cost half an fp16 step over 32768 tokens.
 //
-// The weights p_t vs_t are two fp16 parts, an A operand each, 22 bits together
-// while they are above 2^-14.  So the reference m that is taken off the scores x
-// (log2 units) follows the weights and not the scores: it makes the first step's
-// largest weight 1 whatever the values' scale is, and moves when a weight passes
-// 2^15.  (Scales below 2^-24, none but 0 in fp16, count as that, so that rows of
-// equal values have a reference.)
+// The weights p_t vs_t are two fp16 parts, an A operand each: the first truncated,
+// the second what that leaves, to nearest (truncated as well, the products would be
+// low and the zeros' sum would not, an offset of all outputs).  Together they are off
+// by 2^-21 of the weight, or by 2^-25 where that is more.  So the reference m that is
+// taken off the scores x (log2 units) follows the weights and not the scores: it makes
+// the first step's largest weight 2^8 whatever the values' scale is, so that 2^-25 is
+// 2^-33 of it, and moves when a weight passes 2^15.  (At 2^12 it moves so often that
+// one sequence of 32768 takes 19.9 us instead of 18.8; at 1, 6000 tokens that together
+// have 1% of the weight beside one of value 0 lost all of it to truncation.  Scales
+// below 2^-24, none but 0 in fp16, count as that, so that rows of equal values have a
+// reference.)
 //
 // Where a row is several groups, a key's constants belong to its elements and not to
 // its score: keys and values enter as RN16(code * scale + zero), the weights
@@ -1252,7 +1257,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
                                         : x[u][r] + __builtin_amdgcn_logf(
                                                         fmaxf((float)vsh[u][r], 0x1p-24f)));
             y = lane_max<4>(y);
-            y = lane_max<5>(y);
+            y = lane_max<5>(y) - (NG == 1 ? 8.0f : 0.0f);
             const float mn = fmaxf(m, ms + y);
             const float up = (mn > -inf ? mn : 0.0f) - ms;
             const float f = m > -inf ? __builtin_amdgcn_exp2f(-up) : 0.0f;
@@ -1287,12 +1292,11 @@ __global__ __launch_bounds__(64 * ROWS_W)
                     hh[2 * u + r / 2] = __builtin_bit_cast(uint32_t, w2);
                     continue;
                 }
-                // the first part truncated, the second what that leaves
                 const h2v hi = pk_rtz(wt[u][r], wt[u][r + 1]);
+                const h2v lo = {(_Float16)__builtin_fmaf((float)hi[0], -1.0f, wt[u][r]),
+                                (_Float16)__builtin_fmaf((float)hi[1], -1.0f, wt[u][r + 1])};
                 hh[2 * u + r / 2] = __builtin_bit_cast(uint32_t, hi);
-                ll[2 * u + r / 2] = __builtin_bit_cast(
-                    uint32_t, pk_rtz(__builtin_fmaf((float)hi[0], -1.0f, wt[u][r]),
-                                     __builtin_fmaf((float)hi[1], -1.0f, wt[u][r + 1])));
+                ll[2 * u + r / 2] = __builtin_bit_cast(uint32_t, lo);
             }
         const v8h wh = __builtin_bit_cast(v8h, make_uint4(hh[0], hh[1], hh[2], hh[3]));
         const v8h wl = NG > 1 ? v8h{} : __builtin_bit_cast(v8h, make_uint4(ll[0], ll[1], ll[2], ll[3]));
