@@ -15,7 +15,8 @@
 // B operand of O = V^T P^T: the weights never leave their registers.  Softmax
 // sums and outputs are binary32.  Three roundings to fp16 come on top of the
 // output's own: keys, values, and weights for their product.  Each is off by half
-// a step at most and at random, so that an output of many tokens is off by about
+// a step at most (a weight, where that is less, by 2^-31 of the row's largest) and at
+// random, so that an output of many tokens is off by about
 // 5e-4 of its size instead of 2e-4; taking the codes as they are and the weights
 // in two parts, as k_paged_rows does, would be half as many matrix products again
 // where these are what bounds the kernel.
@@ -42,6 +43,13 @@ typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
+
+// Log2 of a row's largest weight when its softmax reference is taken.  fp16's smallest
+// numbers, and so the error of small weights, are as far below it as they can be; but
+// the reference moves when weights pass 2^15, and nearer to that it does so more often
+// (a prompt of 8192: 1212 us at 0, 1218 at 6, 1229 at 8; single tokens the same for 0
+// and 8, a twentieth more for 12).
+constexpr float TOP_TILE = 6.0f, TOP_ROWS = 8.0f;
 
 // What a block of MR query rows works on.
 struct Work : paged::Span {
@@ -666,7 +674,7 @@ __global__ __launch_bounds__(64 * NW)
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt),
                                                              __float_as_uint(mt), false, false);
             const float mn =
-                fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2);
+                fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2 - TOP_TILE);
             const float ms = mn > -inf ? mn : 0.0f;  // nothing seen so far: weights 0
             const float f = m > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.0f;
             m = mn;
@@ -953,7 +961,7 @@ __global__ __launch_bounds__(64 * NW)
 //
 // Where a row is several groups, a key's constants belong to its elements and not to
 // its score: keys and values enter as RN16(code * scale + zero), the weights
-// rounded to fp16, as in the tiles, and m is the largest score's.  (16 sequences
+// rounded to fp16, as in the tiles, and m makes the largest score's weight 2^8.  (16 sequences
 // over up to 8192 tokens, 32 heads on 8: 36 us with groups of 128, 39 of 64, 40 of
 // 32; by 64-row tiles 142.)
 //
@@ -1257,7 +1265,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
                                         : x[u][r] + __builtin_amdgcn_logf(
                                                         fmaxf((float)vsh[u][r], 0x1p-24f)));
             y = lane_max<4>(y);
-            y = lane_max<5>(y) - (NG == 1 ? 8.0f : 0.0f);
+            y = lane_max<5>(y) - TOP_ROWS;
             const float mn = fmaxf(m, ms + y);
             const float up = (mn > -inf ? mn : 0.0f) - ms;
             const float f = m > -inf ? __builtin_amdgcn_exp2f(-up) : 0.0f;

@@ -61,3 +61,23 @@ def test_two_part_weights(dev, orc, D, bits):
     tol = np.abs(ref) * 2.0 ** -11 + 2.0 ** -25 + \
         mass * (2.0 ** -21 + binary32(n, bits)) + n * 15 * 2.0 ** -33
     assert (np.abs(got - ref) / tol).max() <= 1
+
+
+@pytest.mark.parametrize("bits", [19, 16])
+@pytest.mark.parametrize("new,H,hkv,D,G", [
+    (2, 8, 1, 128, 32), (4, 4, 1, 64, 32), (3, 4, 1, 256, 64),                    # few rows, groups
+    (40, 1, 1, 128, 128), (30, 4, 1, 128, 64), (64, 8, 2, 128, 128),              # tiles
+    (50, 1, 1, 64, 64), (100, 4, 1, 64, 32), (60, 2, 1, 256, 256), (70, 1, 1, 256, 128)])
+def test_one_part_weights(dev, orc, new, H, hkv, D, G, bits):
+    """Weights rounded to fp16 are off by half a step, 2^-11 of themselves, or by half of
+    fp16's smallest number, 2^-25, where that is more: the largest starts at 2^6 or more,
+    of which it is 2^-31."""
+    n = 6000
+    bt, qh, at, first = one_large(new + D + bits, n, new, H, hkv, D, G, bits, 0.0)
+    c, s, z = bt.v
+    z[at], c[first], s[at] = 0, 0, 0.5
+    got = attend(dev, bt, qh, max_seq_len=1)
+    ref = orc.paged_attention(qh, bt.k, bt.v, bt.table, bt.lens, bt.cu, G)
+    # all values are 0 or more, so the sums are the outputs
+    tol = np.abs(ref) * (2 * 2.0 ** -11 + binary32(n, bits)) + 2.0 ** -25 + n * 7.5 * 2.0 ** -31
+    assert (np.abs(got - ref) / tol).max() <= 1
