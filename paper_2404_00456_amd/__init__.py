@@ -925,12 +925,14 @@ def _new(shape, dtype, dev, stream: Optional[torch.cuda.Stream]):
         return torch.empty(shape, dtype=dtype, device=dev)
 
 
-def _on_device(dev, **tensors):
-    """Every tensor on `dev`, and `dev` the current device (whose stream the
-    call runs on)."""
+def _on_device(dev, stream: Optional[torch.cuda.Stream] = None, **tensors):
+    """Every tensor and the stream on `dev`, and `dev` the current device (whose
+    current stream is taken where there is none)."""
     if dev.type == "cuda" and dev.index != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on {dev}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"stream must be on {dev}, got one of {stream.device}")
     for name, t in tensors.items():
         if t is not None and t.device != dev:
             raise ValueError(f"{name} must be on {dev}, got {t.device}")
@@ -1035,7 +1037,7 @@ def quarot_rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor
     _shape(y, x.shape, "y")
     T, H, D = x.shape
     r = _rotary(positions, inv_freq, sections, interleaved, T, D)
-    _on_device(x.device, positions=positions, inv_freq=inv_freq, y=y)
+    _on_device(x.device, stream, positions=positions, inv_freq=inv_freq, y=y)
     if y is None:
         y = _new((T, H, D), torch.float16, x.device, stream)
     (xp, xs), (yp, ys) = _token_rows(x, "x"), _token_rows(y, "y")
@@ -1076,7 +1078,7 @@ def quarot_kv_append_paged(k: torch.Tensor, v: torch.Tensor, k_cache, v_cache,
     r = None
     if inv_freq is not None:
         r = _rotary(positions, inv_freq, sections, interleaved, T, D)
-    _on_device(k_cache[0].device, k=k, v=v, q=q, q_out=q_out, positions=positions,
+    _on_device(k_cache[0].device, stream, k=k, v=v, q=q, q_out=q_out, positions=positions,
                inv_freq=inv_freq)
     if q is not None and q_out is None:
         q_out = _new((T, H, D), torch.float16, q.device, stream)
@@ -1118,7 +1120,7 @@ def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: tor
     T, H, D = q.shape
     _shape(out, q.shape, "out")
     cache = _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group, q, "q", False)
-    _on_device(k_cache[0].device, q=q, out=out, workspace=workspace)
+    _on_device(k_cache[0].device, stream, q=q, out=out, workspace=workspace)
     if max_seq_len is None:
         max_seq_len = cache.max_pages * cache.page_size
     if sm_scale is None:
