@@ -613,7 +613,8 @@ quarot_status quarot_kv_append_paged(const quarot_f16 *q, int64_t q_stride, quar
 
 /*
  * Bytes of device workspace quarot_kv_paged_attention needs (0: none).
- * Host-only; 0 for invalid sizes.
+ * Host-only; 0 for sizes that the call refuses.  (No size depends on group,
+ * which is only checked.)
  */
 size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_t n_heads,
                                                 int64_t n_kv_heads, int64_t head_dim,

@@ -21,6 +21,11 @@ bool head_dim_ok(int64_t d)
     return d == 64 || d == 128 || d == 256;
 }
 
+bool group_ok(int64_t group, int64_t d)
+{
+    return group >= 32 && group <= d && !(group & (group - 1));
+}
+
 quarot_status check_stride(int64_t stride, int64_t heads, int64_t D)
 {
     if (stride < heads * D)
@@ -63,8 +68,7 @@ quarot_status check_cache_sizes(const quarot_paged_kv *c, int64_t T)
     if (!c || T < 0 || c->batch <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->group <= 0 ||
         c->n_pages <= 0 || c->page_size <= 0 || c->max_pages <= 0)
         return QUAROT_ERR_INVALID_ARG;
-    if (!head_dim_ok(c->head_dim) || c->group < 32 || c->group > c->head_dim ||
-        (c->group & (c->group - 1)) || c->page_size % 16 || c->page_size > kMaxTokens ||
+    if (!head_dim_ok(c->head_dim) || !group_ok(c->group, c->head_dim) || c->page_size % 16 || c->page_size > kMaxTokens ||
         c->max_pages > kMaxTokens / c->page_size || c->n_pages > 0x7FFFFFFF ||
         c->n_kv_heads > 0xFFFF || c->batch > 0xFFFFFF || T > kMaxTokens)
         return QUAROT_ERR_UNSUPPORTED_SIZE;
@@ -96,6 +100,16 @@ void fill_cache(const quarot_paged_kv *c, int64_t T, PagedPool &k, PagedPool &v,
     m.n_pages = (int)c->n_pages;
     m.page = (int)c->page_size;
     m.div = paged::divisor(m.page);
+}
+
+// A launch holds fewer than 2^32 threads.
+bool plan_fits(const paged::Plan &p, int64_t T, int64_t batch, int64_t hkv, int64_t rep)
+{
+    for (int i = 0; i < p.n; ++i)
+        if (paged::slots(p.part[i], T, batch, rep) * hkv * p.part[i].splits >
+            0xFFFFFFFFll / paged::MAX_THREADS)
+            return false;
+    return true;
 }
 
 // The launches of a plan use the workspace one after the other.
@@ -215,13 +229,17 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
                                                 int64_t n_sinks)
 {
     if (T <= 0 || T > kMaxTokens || batch <= 0 || batch > 0xFFFFFF || n_heads <= 0 ||
-        n_heads > 0xFFFF || n_kv_heads <= 0 || n_heads % n_kv_heads || !head_dim_ok(head_dim) ||
-        group <= 0 || max_seq_len <= 0 || window < 0 || n_sinks < 0)
+        n_heads > 0xFFFF || T * n_heads > kMaxTokens || n_kv_heads <= 0 || n_heads % n_kv_heads ||
+        !head_dim_ok(head_dim) || !group_ok(group, head_dim) || max_seq_len <= 0 || window < 0 ||
+        n_sinks < 0)
         return 0;
-    const paged::Plan p = paged::plan(T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim,
-                                   std::min(max_seq_len, kMaxTokens), std::min(window, kMaxTokens),
-                                   std::min(n_sinks, kMaxTokens));
-    return attention_workspace(p, T, batch, n_kv_heads, n_heads / n_kv_heads, head_dim);
+    const int64_t rep = n_heads / n_kv_heads;
+    const paged::Plan p = paged::plan(T, batch, n_kv_heads, rep, head_dim,
+                                      std::min(max_seq_len, kMaxTokens), std::min(window, kMaxTokens),
+                                      std::min(n_sinks, kMaxTokens));
+    return plan_fits(p, T, batch, n_kv_heads, rep)
+               ? attention_workspace(p, T, batch, n_kv_heads, rep, head_dim)
+               : 0;
 }
 
 quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, quarot_f16 *out,
@@ -254,10 +272,8 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
     const int64_t hkv = cache->n_kv_heads, rep = n_heads / hkv;
     const paged::Plan p = paged::plan(T, cache->batch, hkv, rep, D,
                                       std::min(max_seq_len, kMaxTokens), window, n_sinks);
-    for (int i = 0; i < p.n; ++i)  // a launch holds fewer than 2^32 threads
-        if (paged::slots(p.part[i], T, cache->batch, rep) * hkv * p.part[i].splits >
-            0xFFFFFFFFll / paged::MAX_THREADS)
-            return QUAROT_ERR_UNSUPPORTED_SIZE;
+    if (!plan_fits(p, T, cache->batch, hkv, rep))
+        return QUAROT_ERR_UNSUPPORTED_SIZE;
     const size_t need = attention_workspace(p, T, cache->batch, hkv, rep, D);
     if (need && (!workspace || workspace_bytes < need))
         return QUAROT_ERR_WORKSPACE;

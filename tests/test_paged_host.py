@@ -256,6 +256,29 @@ def test_workspace_size_of_bad_sizes():
     assert f(1 << 30, 1, 65535, 1, 128, 1 << 62) >= 0
 
 
+@pytest.mark.parametrize("T,batch,n_heads,n_kv_heads,D,group,most", [
+    (8, 2, 8, 2, 128, g, 30000) for g in (1, 16, 31, 32, 48, 64, 96, 128, 256, 1 << 40)] + [
+    (8, 2, 8, 2, 64, 128, 30000), (8, 2, 8, 2, 256, 256, 30000),
+    (1 << 27, 2, 8, 2, 128, 128, 64), ((1 << 27) + 1, 2, 8, 2, 128, 128, 64),  # T * n_heads
+    (1, 0xFFFFFF, 64, 64, 128, 128, 64), (1, 0xFFFFFF, 1, 1, 128, 128, 64),  # blocks
+    (64, 64, 65535, 65535, 128, 128, 64), (1, 1, 65535, 65535, 128, 128, 1 << 20)])
+def test_workspace_size_and_call_agree(T, batch, n_heads, n_kv_heads, D, group, most):
+    """The query answers 0 for what the call refuses, and what the call needs for
+    the rest."""
+    size = q.quarot_kv_paged_attention_workspace_size(T, batch, n_heads, n_kv_heads, D, most, group=group)
+
+    def call(bytes_):
+        c = cache(batch=batch, n_kv_heads=n_kv_heads, head_dim=D, group=group)
+        return q.lib().quarot_kv_paged_attention(P, n_heads * D, P, n_heads * D, c, T, n_heads, most, 0,
+                                                 0, 0.1, P if bytes_ else None, bytes_, None)
+    if size:
+        assert call(0) == call(size - 1) == WORKSPACE
+    if has_gpu():  # (the pointers are fake)
+        return
+    st = call(size)
+    assert st == NODEV or (st in (INVALID, UNSUPPORTED) and size == 0)
+
+
 def test_injected_error(monkeypatch):
     L = q.lib()
     for name, call in (
