@@ -85,3 +85,32 @@ def attention_tolerance(batch, q, exact, sm_scale=None):
     if not exact:
         tol += (2 * S + 1) * half_step()
     return V * tol
+
+
+# How far outputs may be off on average, relative to their own size.  A rounding to
+# fp16 is off by 2^-10 / sqrt(12) = 2.8e-4 of a value at most as a root mean square
+# (just above a power of two).  Few rows of one group: the output's alone.  Otherwise
+# the weights' as well, and where they are not exact the values' and, through scores
+# of about standard size, the keys': four alike, 5.6e-4.
+ONE_ROUNDING, FOUR_ROUNDINGS = 4e-4, 1e-3
+
+
+def few_rows(batch, H):
+    """Whether the plan takes codes and weights unrounded (16 query rows of a
+    sequence at most, one group a row)."""
+    rep = H // batch.hkv
+    rows = max(batch.new) * rep if len(batch.new) > 1 else batch.T * rep
+    return batch.G == batch.D and rows <= 16
+
+
+def relative_rms(batch, got, ref):
+    """Largest root mean square error of a sequence's queries of one head, relative
+    to that of the outputs themselves (an output of zeros has to be that)."""
+    worst = 0.0
+    for b in range(len(batch.new)):
+        rows = slice(batch.cu[b], batch.cu[b + 1])
+        e = np.sqrt(((got[rows].astype(np.float64) - ref[rows]) ** 2).sum((0, 2)))
+        r = np.sqrt((ref[rows] ** 2).sum((0, 2)))
+        assert (e[r == 0] == 0).all()
+        worst = max(worst, (e[r > 0] / r[r > 0]).max(initial=0.0))
+    return worst
