@@ -94,3 +94,22 @@ def test_keys_of_unseen_tokens(dev, orc, new, total, H, hkv, D, G, page, window,
     got = attend(dev, bt, qh, window=window, n_sinks=sinks).astype(np.float64)
     assert np.isfinite(got[hidden]).all() and not np.isfinite(got[~hidden]).any()
     assert np.abs(got[hidden] - ref[hidden]).max() <= tol
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("new,total,H,hkv,D,G,page,window,sinks", FORMS)
+def test_queries_that_are_not_finite(dev, orc, new, total, H, hkv, D, G, page, window, sinks, bad):
+    """One element of some queries that is not finite: their outputs are not, and no
+    other query's changes."""
+    bt = Batch(11 * D + G + H, new, total, hkv, D, G, page, behind=1)
+    qh = bt.queries(H)
+    tol = attention_tolerance(bt, qh, True)
+    ref = orc.paged_attention(qh, bt.k, bt.v, bt.table, bt.lens, bt.cu, G, window, sinks,
+                              out=np.full(qh.shape, 9.0))
+    hit = np.zeros((bt.T, H), bool)
+    for b, n in enumerate(new):
+        hit[bt.cu[b] + n // 2, b % H] = hit[bt.cu[b + 1] - 1, H - 1] = True
+    qh[hit, D // 3] = bad
+    got = attend(dev, bt, qh, window=window, n_sinks=sinks).astype(np.float64)
+    assert not np.isfinite(got[hit]).any() and np.isfinite(got[~hit]).all()
+    assert np.abs(got[~hit] - ref[~hit]).max() <= tol
