@@ -625,8 +625,9 @@ size_t quarot_kv_paged_attention_workspace_size(int64_t T, int64_t batch, int64_
  * Attention of the new tokens over the pages (§4 Stage 2c with App. A.10's
  * cache; prompts, chunks of prompts and single tokens in one call).  The query
  * at position p sees the cached tokens t <= p with
- *   window == 0  or  t > p - window  or  t < n_sinks,
- * and out = RN16(softmax_t(sm_scale * q . khat_t) . vhat), khat and vhat the
+ *   window == 0  or  t > p - window  or  t < n_sinks
+ * (keys with the rotary positions that they were appended with, in windows and as
+ * sinks), and out = RN16(softmax_t(sm_scale * q . khat_t) . vhat), khat and vhat the
  * dequantized rows, sums and softmax in binary32.  At most 16 query rows a
  * sequence (new tokens times query heads of a cache head; where batch is 1, T
  * counts) with one group a row take codes as they are and weights in two fp16

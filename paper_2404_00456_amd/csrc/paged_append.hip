@@ -7,9 +7,9 @@
 // binary64, one pair per thread, and their cosines and sines left in LDS for
 // all heads.  A row is read a pass ahead of its turn.
 //
-// Bound: HBM.  16384 tokens of 64 heads of 128 take 100 us, 5.4 TB/s, which is what
-// a copy of as many bytes reaches; ragged prompts of up to 4099 tokens with 64
-// query and 8 cache heads 84 us.  A single token is its launch and five memory
+// Bound: HBM.  16384 tokens of 64 heads of 128 take 97 to 114 us from card to card,
+// 4.7 .. 5.5 TB/s, which is what a copy of as many bytes reaches; ragged prompts of up
+// to 4099 tokens with 64 query and 8 cache heads 85 to 94.  A single token is its launch and five memory
 // latencies, 3.7 us.
 #include "paged.hpp"
 #include "quant_math.hpp"

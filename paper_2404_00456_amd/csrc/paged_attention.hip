@@ -22,10 +22,10 @@
 // where these are what bounds the kernel.
 //
 // What bounds it: 32 rows by 32 tokens by 128 dimensions are 16 matrix
-// instructions of 32 cycles, about 115 vector instructions (softmax 60, staging
+// instructions of 32 cycles, about 120 vector instructions (softmax 60, staging
 // 40) and 18 KB of LDS traffic, each about half of a SIMD's time when two waves
 // share it, so all three have to run beside each other.  8192 tokens of 64 heads
-// on 8 take 1.14 to 1.24 ms by the card's clock, 890 .. 970 TFLOP/s where a
+// on 8 take 1.18 to 1.24 ms from card to card, 890 .. 930 TFLOP/s where a
 // library product of 8192^3 reaches 1330.  One wave with 64 rows a SIMD (half the
 // LDS reads) was slower, 1.78 ms: its 512 registers are half accumulators, and
 // the softmax works through copies of them.
@@ -962,14 +962,14 @@ __global__ __launch_bounds__(64 * NW)
 // Where a row is several groups, a key's constants belong to its elements and not to
 // its score: keys and values enter as RN16(code * scale + zero), the weights
 // rounded to fp16, as in the tiles, and m makes the largest score's weight 2^8.  (16 sequences
-// over up to 8192 tokens, 32 heads on 8: 36 us with groups of 128, 39 of 64, 40 of
+// over up to 8192 tokens, 32 heads on 8: 35 us with groups of 128, 38 of 64, 39 of
 // 32; by 64-row tiles 142.)
 //
 // What bounds it: a stage of 32 tokens is 4.3 KB for D = 128 and about 280 vector
 // instructions, 1100 cycles of a SIMD where the memory's share of one takes 2000;
 // but of the 17 us that a block of 1024 tokens takes 7 are its start (sequence,
 // pages, queries, first codes) and its end, which four blocks a CU hide only in
-// part.  64 sequences of 1 .. 8192 tokens: 69 us and 7 for their joining, 277 MB.
+// part.  64 sequences of 1 .. 8192 tokens: 70 us and 6 for their joining, 277 MB.
 // A wave's codes and constants come through a ring of its own in LDS, 32 tokens
 // a stage, by loads that go from memory straight there (16 bytes a lane): the
 // next stage is on its way while this one is multiplied, at no registers, and

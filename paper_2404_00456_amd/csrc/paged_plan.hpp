@@ -183,13 +183,20 @@ inline Plan plan(int64_t T, int64_t B, int64_t hkv, int64_t rep, int64_t D,
     if (rep > FEW_ROWS || (B == 1 && rows > FEW_ROWS))
         return Plan{1, {tile_part(ALL, steps, rows, T, B, hkv, rep, D)}};
     // Sequences of few rows: guessed tokens of 64 sequences, 16 rows each, take 66 us
-    // so and 84 with a launch for longer ones beside; but a batch of single tokens
+    // so and 92 with a launch for longer ones beside; but a batch of single tokens
     // may hold a chunk of all the rest, which the tiles read four times as fast, so
-    // only up to 1024 rows of it.
+    // only up to 1024 rows of it.  (300 sequences with 4 rows a token: 900 tokens of one
+    // over 16384 and a token each of the others 550 us by two launches, 600 so; 3 tokens
+    // each over 2048 lose by it, 163 and 145.)
     if (rows <= FEW_ROWS && most <= 64 * FEW_ROWS)
         return Plan{1, {few_part(ALL, steps, B, hkv)}};
     // Chunks, with single tokens among them maybe: 64 sequences, half of them one
-    // token, 244 us so and 285 in tiles alone, where nothing but chunks loses 4 us.
+    // token, 244 us so and 285 in tiles alone, where nothing but chunks loses 4 us.  The
+    // tiles are for a chunk of up to all the rest, which a quarter of that stands for:
+    // 64 sequences with 8 rows a token over 4096, 193 tokens of one and one each of the
+    // others 155 us so and 210 in tiles for the average.  Short chunks alike have the same
+    // sizes here and pay for it: 4 tokens each 357 us so, 274 by the average, 164 in
+    // blocks of FEW_ROWS rows, which the 193 over 16384 would lose by (244 and 318).
     return Plan{2, {tile_part(MANY, steps, std::max(rows, most / 4), T, B, hkv, rep, D),
                     few_part(FEW, steps, B, hkv)}};
 }
