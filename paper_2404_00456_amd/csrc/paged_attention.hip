@@ -450,7 +450,7 @@ __device__ __forceinline__ PagedAttnArgs args_again()
 // One row of a block by one wave, token by token, a token seen or not touched at
 // all: for blocks of few rows in several groups that hold a value that is not finite
 // and that only some of the rows see, since the products of all rows with all tokens
-// would make 0 times it of the others.  (64 sequences of 4 new tokens: 71 us, 2.5 ms
+// would make 0 times it of the others.  (64 sequences of 4 new tokens: 80 us, 2.6 ms
 // so.)  64 scores at a time, a token a lane; then each seen token's value, D /
 // 64 elements a lane.  The result goes where the block's goes.
 template <int D>
