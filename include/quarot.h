@@ -652,6 +652,37 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
                                         int64_t n_sinks, float sm_scale, void *workspace,
                                         size_t workspace_bytes, void *stream);
 
+/*
+ * The same attention with forms of the scores and of what a query sees, as models have
+ * them that cap their scores, take positions by distance, or see documents and prefixes:
+ *   x_t = sm_scale * q . khat_t,
+ *   x_t = cap tanh(x_t / cap)                  with cap > 0,
+ *   x_t = x_t - slopes[h] |p - t|              with slopes (query head h, any finite value),
+ *   seen: t < min(end[r], seq_lens[b]) and (t >= begin[r] or t < n_sinks), with
+ *         window > 0 also (t > p - window or t < n_sinks),
+ * for the query of batch row r at position p; begin NULL: 0, end NULL: p + 1.  A document
+ * packed among others begins at begin[r]; a prefix whose tokens see each other has end[r] =
+ * max(p + 1, its length), which may lie past p; sinks are then seen by every document.
+ * Neither changes with the other: a query with begin[r] >= end[r] sees its sinks, or
+ * nothing and gives zeros.  All three arrays lie on the device and are read when the
+ * kernels run; any content of begin and end is in bounds.
+ * All else is as in quarot_kv_paged_attention, the workspace (and its query) as well.
+ * cap 0 (none) or 2^-64 .. 2^64.
+ */
+typedef struct quarot_scoring {
+    float cap;
+    const float *slopes;  /* [n_heads] or NULL */
+    const int32_t *begin; /* [T] or NULL */
+    const int32_t *end;   /* [T] or NULL */
+} quarot_scoring;
+
+quarot_status quarot_kv_paged_attention_scored(const quarot_f16 *q, int64_t q_stride, quarot_f16 *out,
+                                               int64_t out_stride, const quarot_paged_kv *cache,
+                                               const quarot_scoring *scoring, int64_t T, int64_t n_heads,
+                                               int64_t max_seq_len, int64_t window, int64_t n_sinks,
+                                               float sm_scale, void *workspace, size_t workspace_bytes,
+                                               void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -53,6 +53,11 @@ class _PagedKV(ctypes.Structure):
                              "max_pages")]
 
 
+class _Scoring(ctypes.Structure):
+    """quarot_scoring of include/quarot.h."""
+    _fields_ = [("cap", _F), ("slopes", _P), ("begin", _P), ("end", _P)]
+
+
 # name -> (restype, argtypes), exactly the declarations of include/quarot.h
 SIGNATURES = {
     "quarot_status_string": (ctypes.c_char_p, [_I]),
@@ -105,6 +110,8 @@ SIGNATURES = {
     "quarot_kv_paged_attention_workspace_size": (ctypes.c_size_t, [_I64] * 9),
     "quarot_kv_paged_attention": (_I, [_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I64, _I64, _F,
                                        _P, ctypes.c_size_t, _P]),
+    "quarot_kv_paged_attention_scored": (_I, [_P, _I64, _P, _I64, _P, _P, _I64, _I64, _I64, _I64,
+                                              _I64, _F, _P, ctypes.c_size_t, _P]),
 }
 
 # name -> (restype, argtypes), exactly the declarations of include/quarot_probe.h
@@ -1103,19 +1110,8 @@ def quarot_kv_paged_attention_workspace_size(T: int, batch: int, n_heads: int, n
         window, n_sinks))
 
 
-def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: torch.Tensor,
-                              seq_lens: torch.Tensor, cu_new: torch.Tensor, group: int = 128,
-                              window: int = 0, n_sinks: int = 0,
-                              max_seq_len: Optional[int] = None,
-                              sm_scale: Optional[float] = None,
-                              out: Optional[torch.Tensor] = None,
-                              workspace: Optional[torch.Tensor] = None,
-                              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """Attention of the new tokens' queries q fp16 [T, n_heads, D] (as
-    quarot_kv_append_paged returns them) over the pages: causal, with a sliding
-    window and sinks where window > 0.  max_seq_len: the longest sequence to
-    plan for (default: what the table holds).  Returns fp16 [T, n_heads, D];
-    rows of no sequence are not written."""
+def _paged_attention(q, k_cache, v_cache, page_table, seq_lens, cu_new, group, window, n_sinks,
+                     max_seq_len, sm_scale, out, workspace, stream, scoring):
     _half_rows(q, "q")
     T, H, D = q.shape
     _shape(out, q.shape, "out")
@@ -1133,12 +1129,61 @@ def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: tor
             T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks, group)
         if need:
             workspace = _new((need,), torch.uint8, q.device, stream)
-    _check("quarot_kv_paged_attention", lib().quarot_kv_paged_attention(
-        qp, qs, op, ost, ctypes.byref(cache), T, H, int(max_seq_len), int(window), int(n_sinks),
-        float(sm_scale),
-        _ptr(workspace, torch.uint8, "workspace") if workspace is not None else None,
-        workspace.numel() if workspace is not None else 0, _stream(stream)))
+    head = (qp, qs, op, ost, ctypes.byref(cache))
+    tail = (T, H, int(max_seq_len), int(window), int(n_sinks), float(sm_scale),
+            _ptr(workspace, torch.uint8, "workspace") if workspace is not None else None,
+            workspace.numel() if workspace is not None else 0, _stream(stream))
+    if scoring is None:
+        _check("quarot_kv_paged_attention", lib().quarot_kv_paged_attention(*head, *tail))
+    else:
+        _check("quarot_kv_paged_attention_scored",
+               lib().quarot_kv_paged_attention_scored(*head, ctypes.byref(scoring), *tail))
     return out
+
+
+def quarot_kv_paged_attention(q: torch.Tensor, k_cache, v_cache, page_table: torch.Tensor,
+                              seq_lens: torch.Tensor, cu_new: torch.Tensor, group: int = 128,
+                              window: int = 0, n_sinks: int = 0,
+                              max_seq_len: Optional[int] = None,
+                              sm_scale: Optional[float] = None,
+                              out: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None,
+                              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries q fp16 [T, n_heads, D] (as
+    quarot_kv_append_paged returns them) over the pages: causal, with a sliding
+    window and sinks where window > 0.  max_seq_len: the longest sequence to
+    plan for (default: what the table holds).  Returns fp16 [T, n_heads, D];
+    rows of no sequence are not written."""
+    return _paged_attention(q, k_cache, v_cache, page_table, seq_lens, cu_new, group, window,
+                            n_sinks, max_seq_len, sm_scale, out, workspace, stream, None)
+
+
+def quarot_kv_paged_attention_scored(q: torch.Tensor, k_cache, v_cache, page_table: torch.Tensor,
+                                     seq_lens: torch.Tensor, cu_new: torch.Tensor,
+                                     group: int = 128, window: int = 0, n_sinks: int = 0,
+                                     max_seq_len: Optional[int] = None,
+                                     sm_scale: Optional[float] = None, cap: float = 0.0,
+                                     slopes: Optional[torch.Tensor] = None,
+                                     begin: Optional[torch.Tensor] = None,
+                                     end: Optional[torch.Tensor] = None,
+                                     out: Optional[torch.Tensor] = None,
+                                     workspace: Optional[torch.Tensor] = None,
+                                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """quarot_kv_paged_attention with scores capped by cap * tanh(x / cap) (cap > 0),
+    less slopes[h] for each position of distance (float32 [n_heads]), and queries that
+    see their own span of tokens: from begin on (the sinks apart), before end (int32
+    [T], positions of their sequence; None: 0, and causal).  Documents packed in a
+    sequence begin where they do; tokens of a prefix that see each other have its
+    length as end, where that is past their own position."""
+    for t, n, name in ((slopes, q.shape[1] if q.dim() == 3 else -1, "slopes"),
+                       (begin, q.shape[0], "begin"), (end, q.shape[0], "end")):
+        if t is not None:
+            _shape(t, (n,), name)
+    _on_device(k_cache[0].device, stream, slopes=slopes, begin=begin, end=end)
+    scoring = _Scoring(float(cap), _ptr(slopes, torch.float32, "slopes"),
+                       _ptr(begin, torch.int32, "begin"), _ptr(end, torch.int32, "end"))
+    return _paged_attention(q, k_cache, v_cache, page_table, seq_lens, cu_new, group, window,
+                            n_sinks, max_seq_len, sm_scale, out, workspace, stream, scoring)
 
 
 __all__ = [
@@ -1156,5 +1201,5 @@ __all__ = [
     "quarot_quant_int4_e3m2", "quarot_linear_e3m2_workspace_size", "quarot_linear_e3m2",
     "quarot_swiglu_quant_e3m2", "prepare_weight_e3m2", "quarot_linear_e3m2_scratch",
     "quarot_rope", "quarot_kv_append_paged", "quarot_kv_paged_attention_workspace_size",
-    "quarot_kv_paged_attention",
+    "quarot_kv_paged_attention", "quarot_kv_paged_attention_scored",
 ]

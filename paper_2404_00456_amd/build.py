@@ -8,6 +8,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -15,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libquarot.so")
 SOURCES = ["capi.cpp", "host_rules.cpp", "rotate_quant.hip", "gemm_w4a4.hip", "gemm_stream.hip",
            "gemm_mid.hip", "gemm_grouped.hip", "kv_attention.hip", "scratch.hip",
-           "capi_paged.cpp", "paged_append.hip", "paged_attention.hip"]
+           "capi_paged.cpp", "paged_append.hip", "paged_attention.hip",
+           "capi_scored.cpp", "paged_scored.hip"]
 # MFMA-only rate probes and the device's peak clock (include/quarot_probe.h)
 PROBE_LIB = os.path.join(HERE, "libquarot_probe.so")
 PROBE_SOURCES = ["probe.hip"]
@@ -61,17 +64,30 @@ def kernel_isa_sha(src: str, symbol: str) -> str:
     return hashlib.sha256(text.encode()).hexdigest()[:16]
 
 
-def _link(sources, lib: str, verbose: bool) -> None:
-    srcs = [os.path.join(CSRC, s) for s in sources]
-    tmp = lib + ".tmp"
-    cmd = [hipcc(), *FLAGS, "-I", os.path.join(ROOT, "include"), *srcs, "-o", tmp]
+def _run(cmd, what: str, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     # hipcc's host pass warns about the device-only target feature: harmless
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed building " + os.path.basename(lib))
+        raise RuntimeError("hipcc failed building " + what)
+
+
+def _link(sources, lib: str, verbose: bool) -> None:
+    """Each source by a compiler of its own, side by side (no device code crosses
+    them), then the library of their objects."""
+    tmp = lib + ".tmp"
+    jobs = max(1, min(len(sources), int(os.environ.get("MAX_JOBS") or os.cpu_count() or 1)))
+    with tempfile.TemporaryDirectory() as d:
+        objs = [os.path.join(d, s + ".o") for s in sources]
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(jobs) as pool:
+            list(pool.map(lambda s, o: _run([hipcc(), *compile_flags, "-I", os.path.join(ROOT, "include"),
+                                             "-c", os.path.join(CSRC, s), "-o", o], s, verbose),
+                          sources, objs))
+        _run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *objs, "-o", tmp],
+             os.path.basename(lib), verbose)
     os.replace(tmp, lib)
 
 

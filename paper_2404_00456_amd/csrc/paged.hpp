@@ -74,6 +74,14 @@ struct PagedAttnArgs {
     float *part_ml;      // [rows, hkv, splits, 2]: maximum (in log2 units), sum
 };
 
+// What the scored form has beside: each may be absent.
+struct ScoredAttnArgs : PagedAttnArgs {
+    float cap;             // of the scores; 0: none
+    const float *slopes;   // [hq]: what a score loses for each position of distance
+    const int32_t *begin;  // [T]: first token that a row sees (sinks apart)
+    const int32_t *end;    // [T]: behind the last one
+};
+
 // Row (head 0) of position t of sequence b in the pools, or -1: no page.  Without
 // a branch, so that it can be scheduled among other work.
 __device__ __forceinline__ int64_t pool_row(const PagedMap &m, int hkv, int b, int t)
@@ -105,5 +113,6 @@ __device__ __forceinline__ void search(const PagedMap &m, int &lo, int &n, Befor
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
 hipError_t launch_paged_attention(const PagedAttnArgs &a, int rows, hipStream_t s);
+hipError_t launch_scored_attention(const ScoredAttnArgs &a, int rows, hipStream_t s);
 
 }  // namespace quarot

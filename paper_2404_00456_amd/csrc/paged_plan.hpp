@@ -57,6 +57,29 @@ struct Span {
     int per, used;   // steps of a split, splits that have any (1 at least)
 };
 
+// The steps of a block whose rows see tokens low .. hi - 1 and the sinks before hi, and
+// their splits.
+QUAROT_HD void share(Span &w, int splits, int least)
+{
+    w.used = (w.steps + least - 1) / least;
+    w.used = w.used < 1 ? 1 : w.used > splits ? splits : w.used;
+    w.per = (w.steps + w.used - 1) / w.used;
+    w.per = w.per > 1 ? w.per : 1;
+    w.used = (w.steps + w.per - 1) / w.per;
+    w.used = w.used > 1 ? w.used : 1;
+}
+
+QUAROT_HD void cut(Span &w, int low, int hi, int cap, int sinks, int splits, int least)
+{
+    w.hi = hi > cap ? cap : hi < 0 ? 0 : hi;
+    w.low = low < 0 ? 0 : low > w.hi ? w.hi : low;
+    w.first = w.low / STEP;
+    w.lo = ((sinks < w.hi ? sinks : w.hi) + STEP - 1) / STEP;
+    w.lo = w.lo < w.first ? w.lo : w.first;
+    w.steps = (w.hi + STEP - 1) / STEP + w.lo - w.first;
+    share(w, splits, least);
+}
+
 // Sequence of rows cu0 .. cu1 - 1 of a batch of T, len cached tokens; block
 // `slot - first_slot` of it; a table of cap positions; window 0: none; at most
 // `splits` equal splits, for each `least` steps one.  Any content of cu0, cu1 and len gives a span inside the
@@ -85,12 +108,7 @@ QUAROT_HD Span span(int cu0, int cu1, int len, int T, int cap, int rep, int64_t 
         w.lo = w.lo < w.first ? w.lo : w.first;
         w.steps += w.lo - w.first;
     }
-    w.used = (w.steps + least - 1) / least;
-    w.used = w.used < 1 ? 1 : w.used > splits ? splits : w.used;
-    w.per = (w.steps + w.used - 1) / w.used;
-    w.per = w.per > 1 ? w.per : 1;
-    w.used = (w.steps + w.per - 1) / w.per;
-    w.used = w.used > 1 ? w.used : 1;
+    share(w, splits, least);
     return w;
 }
 
