@@ -683,6 +683,77 @@ quarot_status quarot_kv_paged_attention_scored(const quarot_f16 *q, int64_t q_st
                                                float sm_scale, void *workspace, size_t workspace_bytes,
                                                void *stream);
 
+/*
+ * ---- The pages of the cache ---------------------------------------------------
+ *
+ * Which page holds what of which sequence, kept on the device:
+ *   page_table int32 [batch, max_pages] and seq_lens int32 [batch] as above (a length
+ *   counts the cached tokens), page_refs int32 [n_pages]: how many entries of the table
+ *   hold a page; 0: it is free.
+ * A table starts with -1 everywhere and references of 0.  Entries that are no page hold
+ * none.  The calls change all three in place; results depend on the arguments alone (the
+ * lowest free page is dealt first, to the lowest sequence and its lowest entry).  One
+ * table serves the pools of all layers: the copies that a call asks for are made with
+ * quarot_kv_pages_copy in each of them, before anything is appended.
+ * batch at most 16384, n_pages at most 2^30, int32 arrays 4-byte aligned and disjoint.
+ */
+
+/* Bytes of device workspace of quarot_kv_pages_reserve and _compact (16-byte aligned; calls
+ * that may run at the same time need one each). */
+size_t quarot_kv_pages_workspace_size(int64_t n_pages);
+
+/*
+ * Every sequence b goes on from where sequence parent[b] was: its entries and its length
+ * become those (parent[b] == b: it stays; any number outside 0 .. batch - 1: it ends, its
+ * entries -1 and its length 0).  Pages are shared, no data moves; pages that nobody holds
+ * any more are free.  Forks, reorders a beam and frees in one launch.
+ *   parent int32 [batch].
+ */
+quarot_status quarot_kv_pages_fork(int32_t *page_table, int32_t *seq_lens, int32_t *page_refs,
+                                   const int32_t *parent, int64_t batch, int64_t max_pages,
+                                   int64_t n_pages, void *stream);
+
+/*
+ * Sequences grow by n_new[b] tokens (or shrink, where it is negative, to 0 at least):
+ * entries on which new tokens fall become pages of their own.  One that is no page gets
+ * a free one; one that others hold as well is replaced by a free one, and where it holds
+ * older tokens too its data has to be copied: page copy_src[b] to page copy_dst[b] (both
+ * -1: none).  Where all that hold such a page grow in this call, the lowest keeps it.  An
+ * entry that should hold older tokens and is no page stays so.  Entries that a sequence
+ * shrinks out of are given back (free for later calls, not in this one).
+ * seq_lens[b] becomes the length with the new tokens, and cu_new [batch + 1] the sums of
+ * the positive n_new, as the append and the attention of these tokens take them.
+ * missing[0] = 0: done.  Else nothing has changed, cu_new is 0 throughout and both copy
+ * lists are -1: missing[0] pages more would have to be free, or (-1) a sequence would
+ * pass its max_pages * page_size positions, or the new tokens 2^30.
+ *   n_new, copy_src, copy_dst int32 [batch]; page_size a multiple of 16.  One launch.
+ */
+quarot_status quarot_kv_pages_reserve(int32_t *page_table, int32_t *seq_lens, int32_t *page_refs,
+                                      const int32_t *n_new, int32_t *cu_new, int32_t *copy_src,
+                                      int32_t *copy_dst, int32_t *missing, int64_t batch,
+                                      int64_t max_pages, int64_t n_pages, int64_t page_size,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The n_live[0] pages that are held get the numbers below that: page move_src[i] becomes
+ * page move_dst[i] (ascending both; -1 behind the last), table and references follow, and
+ * the data has to be copied.  Sources and destinations are disjoint.
+ *   move_src, move_dst int32 [n_pages / 2] (may be NULL with n_pages 1).  Two launches.
+ */
+quarot_status quarot_kv_pages_compact(int32_t *page_table, int32_t *page_refs, int32_t *move_src,
+                                      int32_t *move_dst, int32_t *n_live, int64_t batch,
+                                      int64_t max_pages, int64_t n_pages, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+
+/*
+ * Page src[i] of the pools of `cache` to page dst[i], i < count, keys and values; pairs of
+ * which either is no page are left out.  No page may be a destination twice, or a source
+ * and a destination.  Of `cache` the pools and their sizes are read (no table, lengths, cu_new, batch
+ * or max_pages).  count >= 0 (0 is a no-op).  One launch.
+ */
+quarot_status quarot_kv_pages_copy(const quarot_paged_kv *cache, const int32_t *src, const int32_t *dst,
+                                   int64_t count, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

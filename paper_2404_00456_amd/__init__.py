@@ -112,6 +112,11 @@ SIGNATURES = {
                                        _P, ctypes.c_size_t, _P]),
     "quarot_kv_paged_attention_scored": (_I, [_P, _I64, _P, _I64, _P, _P, _I64, _I64, _I64, _I64,
                                               _I64, _F, _P, ctypes.c_size_t, _P]),
+    "quarot_kv_pages_workspace_size": (ctypes.c_size_t, [_I64]),
+    "quarot_kv_pages_fork": (_I, [_P] * 4 + [_I64] * 3 + [_P]),
+    "quarot_kv_pages_reserve": (_I, [_P] * 8 + [_I64] * 4 + [_P, ctypes.c_size_t, _P]),
+    "quarot_kv_pages_compact": (_I, [_P] * 5 + [_I64] * 3 + [_P, ctypes.c_size_t, _P]),
+    "quarot_kv_pages_copy": (_I, [_P, _P, _P, _I64, _P]),
 }
 
 # name -> (restype, argtypes), exactly the declarations of include/quarot_probe.h
@@ -1186,6 +1191,123 @@ def quarot_kv_paged_attention_scored(q: torch.Tensor, k_cache, v_cache, page_tab
                             n_sinks, max_seq_len, sm_scale, out, workspace, stream, scoring)
 
 
+def _pages(page_table, page_refs, seq_lens=None, **more):
+    """Sequences, entries of each and pages; the addresses of the table, the lengths, the
+    references and `more` (name: (int32 tensor, length))."""
+    _ndim(page_table, 2, "page_table")
+    _ndim(page_refs, 1, "page_refs")
+    B, P = page_table.shape
+    at = [_ptr(page_table, torch.int32, "page_table")]
+    if seq_lens is not None:
+        _shape(seq_lens, (B,), "seq_lens")
+        at.append(_ptr(seq_lens, torch.int32, "seq_lens"))
+    at.append(_ptr(page_refs, torch.int32, "page_refs"))
+    for name, (t, n) in more.items():
+        _shape(t, (n,), name)
+        at.append(_ptr(t, torch.int32, name))
+    return at, B, P, page_refs.shape[0]
+
+
+def quarot_kv_pages_workspace_size(n_pages: int) -> int:
+    """Bytes of workspace of quarot_kv_pages_reserve and quarot_kv_pages_compact."""
+    return int(lib().quarot_kv_pages_workspace_size(n_pages))
+
+
+def _pages_workspace(workspace, n: int, dev, stream):
+    if workspace is None:
+        workspace = _new((quarot_kv_pages_workspace_size(n),), torch.uint8, dev, stream)
+    return workspace, _ptr(workspace, torch.uint8, "workspace"), workspace.numel()
+
+
+def quarot_kv_pages_fork(page_table: torch.Tensor, seq_lens: torch.Tensor, page_refs: torch.Tensor,
+                         parent: torch.Tensor,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Sequence b goes on from where sequence parent[b] (int32 [batch]) was, in place: its
+    row of page_table int32 [batch, max_pages] and its length become those, its pages are
+    shared; with a parent that is no sequence (-1) it ends.  page_refs int32 [n_pages]
+    counts the entries that hold a page (0: free)."""
+    at, B, P, n = _pages(page_table, page_refs, seq_lens, parent=(parent, page_table.shape[0]))
+    _on_device(page_table.device, stream, seq_lens=seq_lens, page_refs=page_refs, parent=parent)
+    _check("quarot_kv_pages_fork", lib().quarot_kv_pages_fork(*at, B, P, n, _stream(stream)))
+
+
+def quarot_kv_pages_reserve(page_table: torch.Tensor, seq_lens: torch.Tensor,
+                            page_refs: torch.Tensor, n_new: torch.Tensor, page_size: int,
+                            cu_new: Optional[torch.Tensor] = None,
+                            copy_src: Optional[torch.Tensor] = None,
+                            copy_dst: Optional[torch.Tensor] = None,
+                            missing: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """Sequences grow by n_new (int32 [batch]; shrink where it is negative), in place, onto
+    pages that nobody else holds.  Returns (cu_new, copy_src, copy_dst, missing): the batch's
+    rows for the append and the attention, the pages to copy in every layer's pools first
+    (quarot_kv_pages_copy; -1: none), and 0, or the pages that were lacking (-1: positions),
+    where nothing has changed and cu_new is 0."""
+    B, dev = page_table.shape[0], page_table.device
+    out = [_new((m,), torch.int32, dev, stream) if t is None else t
+           for t, m in ((cu_new, B + 1), (copy_src, B), (copy_dst, B), (missing, 1))]
+    at, B, P, n = _pages(page_table, page_refs, seq_lens, n_new=(n_new, B), cu_new=(out[0], B + 1),
+                         copy_src=(out[1], B), copy_dst=(out[2], B), missing=(out[3], 1))
+    _on_device(dev, stream, seq_lens=seq_lens, page_refs=page_refs, n_new=n_new, cu_new=out[0],
+               copy_src=out[1], copy_dst=out[2], missing=out[3], workspace=workspace)
+    workspace, ws, size = _pages_workspace(workspace, n, dev, stream)
+    _check("quarot_kv_pages_reserve", lib().quarot_kv_pages_reserve(
+        *at, B, P, n, int(page_size), ws, size, _stream(stream)))
+    return tuple(out)
+
+
+def quarot_kv_pages_compact(page_table: torch.Tensor, page_refs: torch.Tensor,
+                            move_src: Optional[torch.Tensor] = None,
+                            move_dst: Optional[torch.Tensor] = None,
+                            n_live: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """The pages that are held get the lowest numbers, in place.  Returns (move_src,
+    move_dst, n_live): the pages to copy in every layer's pools (int32 [n_pages / 2], -1
+    behind the last), and how many are held."""
+    dev, n = page_table.device, page_refs.shape[0]
+    out = [_new((m,), torch.int32, dev, stream) if t is None else t
+           for t, m in ((move_src, n // 2), (move_dst, n // 2), (n_live, 1))]
+    at, B, P, n = _pages(page_table, page_refs, move_src=(out[0], n // 2), move_dst=(out[1], n // 2),
+                         n_live=(out[2], 1))
+    _on_device(dev, stream, page_refs=page_refs, move_src=out[0], move_dst=out[1], n_live=out[2],
+               workspace=workspace)
+    workspace, ws, size = _pages_workspace(workspace, n, dev, stream)
+    _check("quarot_kv_pages_compact", lib().quarot_kv_pages_compact(*at, B, P, n, ws, size,
+                                                                    _stream(stream)))
+    return tuple(out)
+
+
+def quarot_kv_pages_copy(k_cache, v_cache, src: torch.Tensor, dst: torch.Tensor,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Page src[i] of one layer's pools to page dst[i] (int32; -1: none), keys and values.
+    No page may be a destination twice, or both."""
+    kc, ks, kz = k_cache
+    vc, vs, vz = v_cache
+    _ndim(kc, 4, "k_codes")
+    pages, heads, page, half = kc.shape
+    _ndim(ks, 4, "k_scale")
+    if not ks.shape[3]:
+        raise ValueError(f"k_scale must hold groups, got shape {tuple(ks.shape)}")
+    group = 2 * half // ks.shape[3]
+    _group(group, 2 * half)
+    consts = (pages, heads, page, 2 * half // group)
+    _shape(vc, kc.shape, "v_codes")
+    for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
+        _shape(t, consts, nm)
+    _ndim(src, 1, "src")
+    _shape(dst, src.shape, "dst")
+    _on_device(kc.device, stream, k_scale=ks, k_zero=kz, v_codes=vc, v_scale=vs, v_zero=vz, src=src, dst=dst)
+    f16 = torch.float16
+    cache = _PagedKV(_ptr(kc, torch.uint8, "k_codes"), _ptr(ks, f16, "k_scale"), _ptr(kz, f16, "k_zero"),
+                     _ptr(vc, torch.uint8, "v_codes"), _ptr(vs, f16, "v_scale"), _ptr(vz, f16, "v_zero"),
+                     None, None, None, 0, heads, 2 * half, group, pages, page, 0)
+    _check("quarot_kv_pages_copy", lib().quarot_kv_pages_copy(
+        ctypes.byref(cache), _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"), src.shape[0],
+        _stream(stream)))
+
+
 __all__ = [
     "QuarotError", "lib", "probe_lib", "quarot_version", "quarot_device_peaks", "quarot_mfma_probe",
     "quarot_hadamard_factor",
@@ -1202,4 +1324,6 @@ __all__ = [
     "quarot_swiglu_quant_e3m2", "prepare_weight_e3m2", "quarot_linear_e3m2_scratch",
     "quarot_rope", "quarot_kv_append_paged", "quarot_kv_paged_attention_workspace_size",
     "quarot_kv_paged_attention", "quarot_kv_paged_attention_scored",
+    "quarot_kv_pages_workspace_size", "quarot_kv_pages_fork", "quarot_kv_pages_reserve",
+    "quarot_kv_pages_compact", "quarot_kv_pages_copy",
 ]
