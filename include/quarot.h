@@ -754,6 +754,33 @@ quarot_status quarot_kv_pages_compact(int32_t *page_table, int32_t *page_refs, i
 quarot_status quarot_kv_pages_copy(const quarot_paged_kv *cache, const int32_t *src, const int32_t *dst,
                                    int64_t count, void *stream);
 
+/*
+ * ---- Sampling -------------------------------------------------------------------
+ *
+ * The next token of each row of logits.  With m the row's largest logit and T its
+ * temperature, a token's weight is w = exp((l - m) / T).  Tokens are put in the order of
+ * their logits, the lower index first where they are equal, and
+ *   top_k > 0   keeps the first top_k,
+ *   top_p < 1   of those the shortest beginning whose weights sum up to top_p of theirs
+ *               (one token at least),
+ *   min_p > 0   of those the ones with w >= min_p (at least those of weight 1).
+ * The token is the first in the order of the vocabulary at which the sum of the kept
+ * weights passes u times their total, for a given random number 0 <= u < 1 (others are
+ * taken as 0, or as the last kept token).  T <= 0 (or not a number): the token of the
+ * largest logit, the lowest such.  Logits of -inf or that are no number are never chosen;
+ * a row of nothing else gives -1.  Where some are +inf, those alone have a weight.
+ * Weights are rounded to multiples of 2^-min(51, 62 - ceil(log2 vocab)) and summed
+ * exactly, so that the result does not depend on the order of any sum.
+ *   logits [rows, vocab], `stride` elements between rows, binary16 (f32 == 0) or binary32,
+ *   aligned to an element; u, temperature, top_p, min_p float [rows], top_k int32 [rows],
+ *   each but u may be NULL (temperature 1, the others off); tokens int32 [rows].
+ * rows >= 0 (0 is a no-op); vocab at most 2^20.  One launch, no workspace.
+ */
+quarot_status quarot_sample(const void *logits, int64_t stride, int f32, const float *u,
+                            const float *temperature, const int32_t *top_k, const float *top_p,
+                            const float *min_p, int32_t *tokens, int64_t rows, int64_t vocab,
+                            void *stream);
+
 #ifdef __cplusplus
 }
 #endif

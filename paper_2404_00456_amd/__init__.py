@@ -117,6 +117,7 @@ SIGNATURES = {
     "quarot_kv_pages_reserve": (_I, [_P] * 8 + [_I64] * 4 + [_P, ctypes.c_size_t, _P]),
     "quarot_kv_pages_compact": (_I, [_P] * 5 + [_I64] * 3 + [_P, ctypes.c_size_t, _P]),
     "quarot_kv_pages_copy": (_I, [_P, _P, _P, _I64, _P]),
+    "quarot_sample": (_I, [_P, _I64, _I, _P, _P, _P, _P, _P, _P, _I64, _I64, _P]),
 }
 
 # name -> (restype, argtypes), exactly the declarations of include/quarot_probe.h
@@ -1308,6 +1309,42 @@ def quarot_kv_pages_copy(k_cache, v_cache, src: torch.Tensor, dst: torch.Tensor,
         _stream(stream)))
 
 
+def quarot_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                  top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                  min_p: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The next token of each row of logits fp16 or float32 [rows, vocab] (rows may be
+    strided) from the random numbers u float32 [rows] in [0, 1): temperature (<= 0: the
+    largest logit), top_p, min_p float32 [rows], top_k int32 [rows]; None: temperature 1, no
+    limit.  Returns tokens int32 [rows], -1 for rows of nothing but -inf."""
+    _ndim(logits, 2, "logits")
+    if logits.dtype not in (torch.float16, torch.float32):
+        raise TypeError(f"logits must be {torch.float16} or {torch.float32}, got {logits.dtype}")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    rows, V = logits.shape
+    stride = logits.stride(0) if rows > 1 else V
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError(f"logits: a row must be contiguous, got strides {logits.stride()}")
+    if rows > 1 and stride < V:
+        raise ValueError(f"logits: rows must not overlap, got strides {logits.stride()}")
+    for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p),
+                    ("min_p", min_p), ("tokens", tokens)):
+        _shape(t, (rows,), name)
+    _on_device(logits.device, stream, u=u, temperature=temperature, top_k=top_k, top_p=top_p,
+               min_p=min_p, tokens=tokens)
+    if u is None:
+        raise TypeError("u must be a torch.Tensor")
+    if tokens is None:
+        tokens = _new((rows,), torch.int32, logits.device, stream)
+    f32, i32 = torch.float32, torch.int32
+    _check("quarot_sample", lib().quarot_sample(
+        logits.data_ptr(), stride, int(logits.dtype == f32), _ptr(u, f32, "u"),
+        _ptr(temperature, f32, "temperature"), _ptr(top_k, i32, "top_k"), _ptr(top_p, f32, "top_p"),
+        _ptr(min_p, f32, "min_p"), _ptr(tokens, i32, "tokens"), rows, V, _stream(stream)))
+    return tokens
+
+
 __all__ = [
     "QuarotError", "lib", "probe_lib", "quarot_version", "quarot_device_peaks", "quarot_mfma_probe",
     "quarot_hadamard_factor",
@@ -1325,5 +1362,5 @@ __all__ = [
     "quarot_rope", "quarot_kv_append_paged", "quarot_kv_paged_attention_workspace_size",
     "quarot_kv_paged_attention", "quarot_kv_paged_attention_scored",
     "quarot_kv_pages_workspace_size", "quarot_kv_pages_fork", "quarot_kv_pages_reserve",
-    "quarot_kv_pages_compact", "quarot_kv_pages_copy",
+    "quarot_kv_pages_compact", "quarot_kv_pages_copy", "quarot_sample",
 ]

@@ -11,6 +11,7 @@
 // dependent loads (length, entry, reference) of some 500 ns each.
 #include <algorithm>
 
+#include "block_scan.hpp"
 #include "pages.hpp"
 
 namespace quarot {
@@ -76,29 +77,6 @@ __global__ __launch_bounds__(256) void k_pages_fork(ForkArgs a)
 }
 
 // ---- what the kernels of one block share ------------------------------------
-
-// The sum of v over the threads before this one; `all` the sum of all.
-__device__ __forceinline__ int block_scan(int v, int *sums, int &all)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int x = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        x += lane >= d ? y : 0;
-    }
-    __syncthreads();  // (the last scan's sums are read)
-    if (lane == 63)
-        sums[wave] = x;
-    __syncthreads();
-    int before = 0;
-    all = 0;
-    for (int w = 0; w < WAVES; ++w) {
-        const int s = sums[w];
-        before += w < wave ? s : 0;
-        all += s;
-    }
-    return before + x - v;
-}
 
 // Pages base .. base + NT * PAGES_EACH - 1 of a pool, PAGES_EACH * 64 in a row to each
 // wave: bit k of `yes` of a lane is page first + 64 k + lane.  All loads are on their way
@@ -255,7 +233,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
         int need = copied(b, g) >= 0;
         need += entries(b, g, 0, [](int64_t, int, int) {});
         int all;
-        const int before = total + block_scan(need, sums, all);
+        const int before = total + block_scan<WAVES>(need, sums, all);
         if (b < a.B)
             at[b] = before;
         total += all;
@@ -272,7 +250,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
         const int mine = tile_of(a.refs, base, a.n, yes, [](int, int r) { return r == 0; });
         int all;
         // (a wave's count is the same in its lanes: its first lane brings it)
-        const int before = block_scan(lane == 0 ? mine : 0, sums, all);
+        const int before = block_scan<WAVES>(lane == 0 ? mine : 0, sums, all);
         each_of(base, yes, found + __builtin_amdgcn_readfirstlane(before), [&](int page, int rank) {
             if (rank < total)
                 list[rank] = page;
@@ -288,7 +266,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
         const int b = b0 + tid;
         const Growth g = growth(a, b);
         int all;
-        const int before = cu + block_scan(done ? max(0, g.n) : 0, sums, all);
+        const int before = cu + block_scan<WAVES>(done ? max(0, g.n) : 0, sums, all);
         cu += all;
         int src = -1, dst = -1, rank = 0;
         if (b < a.B && done) {
@@ -356,7 +334,7 @@ __global__ __launch_bounds__(NT) void k_pages_compact(CompactArgs a)
         uint32_t yes;
         const int mine = tile_of(a.refs, base, a.n, yes, [](int, int r) { return r > 0; });
         int all;
-        block_scan(lane == 0 ? mine : 0, sums, all);
+        block_scan<WAVES>(lane == 0 ? mine : 0, sums, all);
         live += all;
     }
     int nsrc = 0, ndst = 0;
@@ -365,8 +343,8 @@ __global__ __launch_bounds__(NT) void k_pages_compact(CompactArgs a)
         const int ms = tile_of(a.refs, base, a.n, from, [&](int i, int r) { return r > 0 && i >= live; });
         const int md = tile_of(a.refs, base, a.n, to, [&](int i, int r) { return r <= 0 && i < live; });
         int alls, alld;
-        const int bs = block_scan(lane == 0 ? ms : 0, sums, alls);
-        const int bd = block_scan(lane == 0 ? md : 0, sums, alld);
+        const int bs = block_scan<WAVES>(lane == 0 ? ms : 0, sums, alls);
+        const int bd = block_scan<WAVES>(lane == 0 ? md : 0, sums, alld);
         each_of(base, from, nsrc + __builtin_amdgcn_readfirstlane(bs), [&](int p, int r) { a.src[r] = p; });
         each_of(base, to, ndst + __builtin_amdgcn_readfirstlane(bd), [&](int p, int r) { a.dst[r] = p; });
         nsrc += alls;
