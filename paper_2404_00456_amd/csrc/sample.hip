@@ -13,11 +13,23 @@
 // vocabulary of 2^17: 2^45), so that a weight that becomes 0 is below 2^-46 of the
 // largest.
 //
-// A block of 16 waves takes a row.  A cut is a search: a histogram over (m - l) / T in
-// equal steps, 2048 of them down to weights of 0, tells in which step it falls; where more
-// than LIST tokens share that, further histograms over the bits of their logits; those
-// that are left are ranked against each other.  Where all of them are equal, the index
-// decides, by counting in the order of the vocabulary.
+// A block of 16 waves takes a row.  What a cut leaves is mostly few tokens: a list of up to
+// LIST of them in LDS, in which the cuts, and the draw, are searches of some tokens a
+// thread.
+//   k      The largest logits of groups of eight, counted by steps of (m - l) / T, give a
+//          logit that k groups reach, and so at least k tokens and hardly more.
+//   p      A histogram of the weights of all tokens by their exponents, in 1/32 of a factor
+//          of 2, gives a logit that the cut does not pass.
+//   min_p  is a least logit.
+// A search sums amounts (ones or weights) in 2048 bins, over the keys of the logits, and
+// divides the bin that holds the target again; few tokens are ranked against each other,
+// equal ones by their numbers.  Rows with more left than a list holds are searched in the
+// same way as a whole, and drawn from by the sums of what is left, by sixteenths of the row
+// and then by tiles of the one that the draw falls in.
+//
+// What bounds it: instructions, of 131072 tokens a microsecond for each one a token of the
+// row's CU.  A pass for the largest logit or for a list is a handful (two fp16 at once, or
+// groups that hold none left out), weighing a token 30, 12 of them in binary64.
 #include <algorithm>
 
 #include "block_scan.hpp"
@@ -30,33 +42,40 @@ constexpr int NT = 1024, WAVES = NT / 64;
 constexpr int BINS = 2048;
 constexpr int TILE = 512;  // elements of a wave's step: 8 a lane
 constexpr int TILES = SAMPLE_MAX_VOCAB / TILE + 1;
-constexpr int LIST = 512;
+constexpr int LIST = 8192;    // tokens in LDS
+constexpr int SOME = 512;     // of them to be ranked
+constexpr int STEPS = 256;    // of a factor of 2 in the table of powers
 
 typedef unsigned long long u64;
 
+template <int N>
+struct Tokens {
+    u64 w[N];
+    float l[N];
+    int at[N];
+};
+
 struct Shared {
-    u64 weight[BINS];  // of a histogram
-    uint32_t count[BINS];
-    u64 tile[TILES];   // sums of the tiles
+    union {
+        u64 bins[BINS];   // a histogram
+        u64 tile[TILES];  // or sums of the tiles
+    };
     u64 sums[WAVES];
-    double pow2[64];   // 2^(i / 64)
-    u64 list_w[LIST];
-    uint32_t list_key[LIST], list_at[LIST];
+    double pow2[STEPS];
+    float edge[2][8];  // the row's first and last eight, where they are not eight
+    Tokens<LIST> list;
+    Tokens<SOME> some;
     uint32_t kmin, kmax, found, bin;
     u64 before;
     int token;
 };
 
-// A logit as the comparisons take it: no -0, and what is not a number as -inf.
-__device__ __forceinline__ float clean(float l)
-{
-    return l == l ? l + 0.0f : -__builtin_inff();
-}
+constexpr float MOST = 0x1.FFFFFEp127f;
 
 // Whole numbers in the order of the logits.
 __device__ __forceinline__ uint32_t key_of(float l)
 {
-    const uint32_t b = __float_as_uint(l);
+    const uint32_t b = __float_as_uint(l + 0.0f);  // (no -0)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
@@ -69,59 +88,138 @@ template <class T>
 struct Row {
     const T *p;
     int V, head, tiles;  // 16-byte loads begin `head` elements before the row
+    const float (*edge)[8];
 
-    __device__ Row(const SampleArgs &a, int64_t row)
+    __device__ Row(const SampleArgs &a, int64_t row, Shared &s)
     {
         p = static_cast<const T *>(a.logits) + row * a.stride;
         V = a.V;
         head = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % (16 / sizeof(T)));
         tiles = (V + head + TILE - 1) / TILE;
+        edge = s.edge;
+        if (threadIdx.x < 16) {  // the eight from -head on, and the last eight
+            const int last = threadIdx.x >> 3, i = (last ? (V + head - 1) / 8 * 8 : 0) + (threadIdx.x & 7) - head;
+            float l = -__builtin_inff();
+            if (i >= 0 && i < V) {
+                if constexpr (sizeof(T) == 2)
+                    l = h2f(p[i]);
+                else
+                    l = p[i];
+            }
+            s.edge[last][threadIdx.x & 7] = l;
+        }
+        __syncthreads();
     }
     __device__ int index(int tile, int e) const
     {
         return tile * TILE + (threadIdx.x & 63) * 8 + e - head;
     }
-    // -inf outside the row
-    __device__ void load(int tile, float (&l)[8]) const
+    struct Raw {
+        uint4 v[sizeof(T) / 2];
+    };
+    __device__ void fetch(int tile, Raw &x) const
+    {
+        const int i = index(tile, 0);
+        if (i >= 0 && i + 8 <= V)
+#pragma unroll
+            for (size_t k = 0; k < sizeof(T) / 2; ++k)
+                x.v[k] = reinterpret_cast<const uint4 *>(p + i)[k];
+    }
+    // As they come (no comparison holds of what is no number); -inf outside the row.
+    __device__ void values(int tile, const Raw &x, float (&l)[8]) const
     {
         const int i = index(tile, 0);
         if (i >= 0 && i + 8 <= V) {
-            if constexpr (sizeof(T) == 2) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(p + i);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t w[2 * sizeof(T)];
+            __builtin_memcpy(w, x.v, sizeof(w));
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    l[e] = clean(h2f((uint16_t)(w[e / 2] >> (16 * (e & 1)))));
-            } else {
-                const float4 a = *reinterpret_cast<const float4 *>(p + i);
-                const float4 b = *reinterpret_cast<const float4 *>(p + i + 4);
-                const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    l[e] = clean(v[e]);
-            }
+            for (int e = 0; e < 8; ++e)
+                l[e] = sizeof(T) == 2 ? h2f((uint16_t)(w[e / 2] >> (16 * (e & 1)))) : __uint_as_float(w[e]);
             return;
         }
+        const bool none = i >= V;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            l[e] = -__builtin_inff();
-            if (i + e >= 0 && i + e < V) {
-                if constexpr (sizeof(T) == 2)
-                    l[e] = clean(h2f(p[i + e]));
-                else
-                    l[e] = clean(p[i + e]);
-            }
+        for (int e = 0; e < 8; ++e)
+            l[e] = none ? -__builtin_inff() : edge[i >= 0][e];
+    }
+    // The largest logit of a lane's eight.
+    __device__ float top(int tile, const Raw &x) const
+    {
+        const int i = index(tile, 0);
+        if (sizeof(T) == 2 && i >= 0 && i + 8 <= V) {
+            typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+            h2v h[4];
+            __builtin_memcpy(h, x.v, sizeof(h));
+            const h2v a = __builtin_elementwise_max(__builtin_elementwise_max(h[0], h[1]),
+                                                    __builtin_elementwise_max(h[2], h[3]));
+            return fmaxf((float)a[0], (float)a[1]);
+        }
+        float l[8];
+        values(tile, x, l);
+        return fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), fmaxf(fmaxf(l[4], l[5]), fmaxf(l[6], l[7])));
+    }
+    __device__ void load(int tile, float (&l)[8]) const
+    {
+        Raw x;
+        fetch(tile, x);
+        values(tile, x, l);
+    }
+    // f(tile, raw) of the tiles of this wave, the next AHEAD of which are on their way (a
+    // row passes by from its XCD's L2 after the first time).  The body stays one copy: with
+    // eight tiles unrolled, a pass that weighs every token waited for its instructions, 115
+    // us for 131072 tokens instead of 33.
+    static constexpr int AHEAD = 16 / (int)sizeof(T) / 2;
+    // of tiles first, first + step, .. before end
+    template <class F>
+    __device__ __forceinline__ void raws(int first, int end, int step, F f) const
+    {
+        Raw x[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (first + k * step < end)
+                fetch(first + k * step, x[k]);
+#pragma unroll 1
+        for (int t = first; t < end; t += step) {
+            const Raw now = x[0];
+#pragma unroll
+            for (int k = 1; k < AHEAD; ++k)
+                x[k - 1] = x[k];
+            if (t + AHEAD * step < end)
+                fetch(t + AHEAD * step, x[AHEAD - 1]);
+            f(t, now);
         }
     }
-    // f(tile, logits) of the tiles of this wave
     template <class F>
-    __device__ void each(F f) const
+    __device__ __forceinline__ void tops(F f) const
     {
-        for (int t = threadIdx.x >> 6; t < tiles; t += WAVES) {
+        raws(threadIdx.x >> 6, tiles, WAVES, [&](int t, const Raw &x) { f(top(t, x)); });
+    }
+    // f(tile, logits)
+    template <class F>
+    __device__ __forceinline__ void each(int first, int end, int step, F f) const
+    {
+        raws(first, end, step, [&](int t, const Raw &x) {
             float l[8];
-            load(t, l);
+            values(t, x, l);
             f(t, l);
-        }
+        });
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        each(threadIdx.x >> 6, tiles, WAVES, f);
+    }
+    // of tiles with a logit of `from` and more
+    template <class F>
+    __device__ __forceinline__ void each_from(float from, F f) const
+    {
+        raws(threadIdx.x >> 6, tiles, WAVES, [&](int t, const Raw &x) {
+            if (!__any(top(t, x) >= from))
+                return;
+            float l[8];
+            values(t, x, l);
+            f(t, l);
+        });
     }
 };
 
@@ -141,58 +239,94 @@ __device__ __forceinline__ float block_max(float v, u64 *sums)
 
 // The weights of a row.
 struct Weights {
-    float m;
-    double step;   // 64 log2(e) / T
+    float m;       // the largest logit, or binary32's where that is infinite
+    double step;   // STEPS log2(e) / T
     float bin;     // bins a unit of logit
-    int one;
-    const double *pow2;
+    const double *pow2;  // 2^(i / STEPS + log2_one)
 
-    // exp((l - m) / T): 2^(n / 64) 2^(r / 64), |r| <= 1/2, the second by the terms of its
-    // series up to the fourth (the fifth is below 4e-14); 0 below 2^-64
+    // exp((l - m) / T) 2^log2_one: 2^(n / STEPS) 2^(r / STEPS), |r| <= 1/2, the second by the
+    // terms of its series up to the third (the fourth is below 2e-13).  n from the last bits
+    // of a sum with 3 2^51.  2^-64 stands for all that is less, and for no number.
+    __device__ __forceinline__ double real(float l, int &n) const
+    {
+        const double x = fmin(fmax(((double)l - (double)m) * step, -64.0 * STEPS), 0.0);
+        const double t = x + 0x1.8p52, r = x - (t - 0x1.8p52);
+        n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+        constexpr double c = 0.693147180559945309417 / STEPS;
+        const double p =
+            __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, c * c * c / 6, c * c / 2), c), 1.0);
+        const double y = pow2[n & (STEPS - 1)] * p;
+        // (far from the ends of the exponent)
+        return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, y) + ((int64_t)(n >> 8) << 52));
+    }
     __device__ __forceinline__ double real(float l) const
     {
-        const double x = l == m ? 0.0 : ((double)l - (double)m) * step;
-        if (!(x > -64.0 * 64.0))
-            return 0.0;
-        const double n = __builtin_rint(x), r = x - n;
-        constexpr double c = 0.693147180559945309417 / 64.0;
-        const double p = __builtin_fma(
-            r, __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, c * c * c * c / 24, c * c * c / 6), c * c / 2), c), 1.0);
-        const int i = (int)n;
-        return __builtin_ldexp(pow2[i & 63] * p, i >> 6);
+        int n;
+        return real(l, n);
     }
-    __device__ __forceinline__ u64 whole(double w) const
+    // to a whole number, by a sum with 2^52
+    __device__ __forceinline__ u64 whole(float l, int &n) const
     {
-        return (u64)__builtin_rint(__builtin_ldexp(w, one));
+        return __builtin_bit_cast(uint64_t, real(l, n) + 0x1p52) & 0xFFFFFFFFFFFFFull;
     }
-    __device__ __forceinline__ u64 operator()(float l) const { return whole(real(l)); }
-    // BINS and more: a weight of 0
+    __device__ __forceinline__ u64 operator()(float l) const
+    {
+        int n;
+        return whole(l, n);
+    }
+    // Bins of the weights: eight steps of the exponent each.
+    __device__ __forceinline__ static int bin_of_step(int n) { return std::min(-n >> 3, BINS - 1); }
+    __device__ __forceinline__ int weight_bin(float l) const
+    {
+        int n;
+        real(l, n);
+        return bin_of_step(n);
+    }
+    // Bins of the logits: equal steps down to weights of 0, which are BINS and more.
     __device__ __forceinline__ int bin_of(float l) const
     {
-        const float x = l == m ? 0.0f : (m - l) * bin;
-        return x < (float)BINS ? (int)x : BINS;
+        const float x = l >= m ? 0.0f : (m - l) * bin;
+        return x < (float)BINS ? (int)x : BINS;  // (0 times infinite: BINS)
     }
 };
 
-// What is left of a row: logits above `cut`, and at it up to index `at`.
+// What is left of a row: logits above `cut`, and at it up to index `at` (-1: none, and
+// EXACT is not needed).
 struct Cut {
     float cut;
     int at;
-    __device__ __forceinline__ bool keeps(float l, int i) const { return l > cut || (l == cut && i <= at); }
+    template <bool EXACT = true>
+    __device__ __forceinline__ bool keeps(float l, int i) const
+    {
+        return EXACT ? l > cut || (l == cut && i <= at) : l > cut;
+    }
 };
 
-// The first bin at which the sum of `of` reaches target, and the sum before it, by all
-// threads; false where it never does.
-template <class T>
-__device__ __forceinline__ bool find(Shared &s, const T *of, u64 target)
+// f(std::bool_constant<EXACT>)
+template <class F>
+__device__ __forceinline__ void with_cut(const Cut &c, F f)
+{
+    if (c.at < 0)
+        f(std::false_type());
+    else
+        f(std::true_type());
+}
+
+// The first bin at which the sum reaches the target, target_of(sum of all), and the sum
+// before it, by all threads; false where it never does.
+template <class F>
+__device__ __forceinline__ bool find(Shared &s, F target_of)
 {
     constexpr int E = BINS / NT;
     u64 mine[E], sum = 0, all;
+#pragma unroll
     for (int e = 0; e < E; ++e) {
-        mine[e] = of[threadIdx.x * E + e];
+        mine[e] = s.bins[threadIdx.x * E + e];
         sum += mine[e];
     }
     u64 before = block_scan<WAVES>(sum, s.sums, all);
+    const u64 target = target_of(all);
+#pragma unroll
     for (int e = 0; e < E; ++e) {
         if (before < target && target <= before + mine[e]) {
             s.bin = threadIdx.x * E + e;
@@ -207,11 +341,40 @@ __device__ __forceinline__ bool find(Shared &s, const T *of, u64 target)
 __device__ __forceinline__ void clear(Shared &s)
 {
     __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += NT) {
-        s.weight[i] = 0;
-        s.count[i] = 0;
+#pragma unroll
+    for (int i = threadIdx.x; i < BINS; i += NT)
+        s.bins[i] = 0;
+    if (threadIdx.x == 0) {
+        s.found = 0;
+        s.kmin = 0xFFFFFFFFu;
+        s.kmax = 0;
     }
     __syncthreads();
+}
+
+// The least logit of which yes() holds, which it does from some logit on and of m: between
+// the keys of -inf and of m, a thousandth of what is left at a time.
+template <class Yes>
+__device__ __forceinline__ float least_logit(Shared &s, float m, Yes yes)
+{
+    uint32_t low = key_of(-__builtin_inff()), high = key_of(m);  // not yet, and already
+#pragma unroll 1
+    while (high - low > 1) {
+        const uint32_t step = (high - low + NT - 1) / NT;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            s.kmin = high;
+        __syncthreads();
+        const uint64_t k = (uint64_t)low + (uint64_t)step * (threadIdx.x + 1);
+        const uint64_t some = __ballot(k < high && yes(of_key((uint32_t)k)));
+        if (some && (threadIdx.x & 63) == (uint32_t)__builtin_ctzll(some))
+            atomicMin(&s.kmin, (uint32_t)k);
+        __syncthreads();
+        high = s.kmin;
+        low = std::max(low, high - step);
+    }
+    __syncthreads();
+    return of_key(high);
 }
 
 // The index of the c-th (from 1) token of the vocabulary with `keeps` (there are as many).
@@ -249,10 +412,7 @@ __device__ int nth(Shared &s, const Row<T> &row, u64 c, Keeps keeps)
         for (int e = 0; e < 8; ++e)
             n += keeps(l[e], row.index(t, e));
         mine = n;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(n, d);
-            n += (int)threadIdx.x >= d ? y : 0;
-        }
+        n = wave_scan(n);
         int left = (int)(c - s.before) - (n - mine);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -265,99 +425,206 @@ __device__ int nth(Shared &s, const Row<T> &row, u64 c, Keeps keeps)
     return at;
 }
 
-// Cuts what is left of a row to its beginning (by logit) whose amounts reach `target`, an
-// amount being 1 or the token's weight.  The histogram of s is that of all that is left.
-template <bool WEIGHTS, class T>
-__device__ void cut_to(Shared &s, const Row<T> &row, const Weights &w, Cut &c, u64 target)
+// What the shortest beginning of a share p sums up to, at least.
+__device__ __forceinline__ u64 share_of(float p, u64 all)
 {
-    auto bins = [&]() { return WEIGHTS ? find(s, s.weight, target) : find(s, s.count, target); };
-    if (!bins())
-        return;
-    // the keys of that bin
-    uint32_t bin = s.bin;
-    target -= s.before;
-    uint32_t n = s.count[bin];
-    if (threadIdx.x == 0) {
-        s.kmin = 0xFFFFFFFFu;
-        s.kmax = 0;
-    }
-    __syncthreads();
-    row.each([&](int t, const float (&l)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (w.bin_of(l[e]) == (int)bin && c.keeps(l[e], row.index(t, e))) {
-                atomicMin(&s.kmin, key_of(l[e]));
-                atomicMax(&s.kmax, key_of(l[e]));
-            }
-    });
-    __syncthreads();
-    uint32_t kmin = s.kmin, kmax = s.kmax;
-    while (n > LIST && kmin < kmax) {
-        const int bits = 32 - __builtin_clz(kmax - kmin), shift = std::max(0, bits - 11);
-        clear(s);
-        row.each([&](int t, const float (&l)[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t k = key_of(l[e]);
-                if (k >= kmin && k <= kmax && c.keeps(l[e], row.index(t, e))) {
-                    atomicAdd(&s.count[(kmax - k) >> shift], 1u);
-                    if (WEIGHTS)
-                        atomicAdd(&s.weight[(kmax - k) >> shift], w(l[e]));
-                }
-            }
-        });
-        __syncthreads();
-        bins();
-        bin = s.bin;
-        target -= s.before;
-        n = s.count[bin];
-        const uint32_t top = kmax - (bin << shift), low = top - ((1u << shift) - 1);
-        kmin = low > kmin && low <= top ? low : kmin;
-        kmax = top;
-    }
-    if (kmin == kmax) {  // equal ones: the first in the order of the vocabulary
-        const float l = of_key(kmin);
-        const u64 each = WEIGHTS ? w(l) : 1;
-        const u64 k = (target + each - 1) / each;
-        const Cut was = c;
-        c.at = nth(s, row, k, [&](float x, int i) { return x == l && was.keeps(x, i); });
-        c.cut = l;
-        return;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0)
-        s.found = 0;
-    __syncthreads();
-    row.each([&](int t, const float (&l)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t k = key_of(l[e]);
-            if (k >= kmin && k <= kmax && c.keeps(l[e], row.index(t, e))) {
-                const uint32_t x = atomicAdd(&s.found, 1u);
-                if (x < LIST) {
-                    s.list_key[x] = k;
-                    s.list_at[x] = row.index(t, e);
-                    s.list_w[x] = WEIGHTS ? w(l[e]) : 1;
-                }
+    const double t = __builtin_ceil((double)p * (double)all);
+    return t < 1.0 ? 1 : std::min((u64)t, all);
+}
+
+// What the sum of the drawn token and those before it is above.
+__device__ __forceinline__ u64 draw(float u, u64 all)
+{
+    const double share = u > 0.0f ? std::min((double)u, 1.0) * (double)all : 0.0;
+    return std::min((u64)share, all - 1);
+}
+
+// The tokens of the list with in(x) and an amount, up to SOME of them, in `some`; how many.
+template <class In, class A>
+__device__ __forceinline__ uint32_t pick(Shared &s, int n, In in, A amount)
+{
+    for (int x = threadIdx.x; x < n; x += NT) {
+        const u64 a = in(x) ? amount(x) : 0;
+        if (a) {
+            const uint32_t y = atomicAdd(&s.found, 1u);
+            if (y < SOME) {
+                s.some.w[y] = a;
+                s.some.l[y] = s.list.l[x];
+                s.some.at[y] = s.list.at[x];
             }
         }
-    });
+    }
     __syncthreads();
-    if (threadIdx.x < n) {
-        const uint32_t k = s.list_key[threadIdx.x], at = s.list_at[threadIdx.x];
-        const u64 mine = s.list_w[threadIdx.x];
-        u64 before = 0;
-        for (uint32_t x = 0; x < n; ++x)
-            before += s.list_key[x] > k || (s.list_key[x] == k && s.list_at[x] < at) ? s.list_w[x] : 0;
-        if (before < target && target <= before + mine) {
-            s.kmin = k;
+    return s.found;
+}
+
+// The first of n tokens of `some`, in the order of their logits or their numbers, at which
+// the sum of their amounts reaches target.
+template <bool BY_NUMBER>
+__device__ __forceinline__ Cut rank(Shared &s, int n, u64 target)
+{
+    if ((int)threadIdx.x < n) {
+        const float l = s.some.l[threadIdx.x];
+        const int at = s.some.at[threadIdx.x];
+        const u64 mine = s.some.w[threadIdx.x];
+        u64 sum = 0;
+        for (int x = 0; x < n; ++x) {
+            const bool first = s.some.at[x] < at;
+            const float y = s.some.l[x];
+            sum += (BY_NUMBER ? first : y > l || (y == l && first)) ? s.some.w[x] : 0;
+        }
+        if (sum < target && target <= sum + mine) {
+            s.kmin = __float_as_uint(l);
             s.token = at;
         }
     }
     __syncthreads();
-    c.cut = of_key(s.kmin);
-    c.at = s.token;
+    return Cut{__uint_as_float(s.kmin), s.token};
+}
+
+// The token of the list, in the order of the numbers, at which the sum of the amounts
+// reaches target_of(their sum), which it does.
+template <class A, class F>
+__device__ __forceinline__ Cut by_number(Shared &s, int n, int V, A amount, F target_of)
+{
+    int shift = 0;
+    while (V > BINS << shift)
+        ++shift;
+    static_assert(SAMPLE_MAX_VOCAB / BINS <= SOME, "the numbers of a bin");
+    clear(s);
+    for (int x = threadIdx.x; x < n; x += NT) {
+        const u64 a = amount(x);
+        if (a)
+            atomicAdd(&s.bins[s.list.at[x] >> shift], a);
+    }
     __syncthreads();
+    u64 target = 0;
+    find(s, [&](u64 all) { return target = target_of(all); });
+    const int b = (int)s.bin;
+    const u64 left = target - s.before;
+    return rank<true>(s, (int)pick(s, n, [&](int x) { return s.list.at[x] >> shift == b; }, amount), left);
+}
+
+// Bits to shift a difference of keys by, so that it is a bin.
+__device__ __forceinline__ int key_shift(uint32_t range)
+{
+    return range ? std::max(0, 32 - __builtin_clz(range) - 11) : 0;
+}
+
+// A bin of keys up to high: what it leaves of low .. high.
+__device__ __forceinline__ void narrow(uint32_t &low, uint32_t &high, uint32_t bin, int shift)
+{
+    high -= bin << shift;
+    const uint32_t first = high - ((1u << shift) - 1);
+    low = first > low && first <= high ? first : low;
+}
+
+// The cut of the list, in the order of the logits, at which the sum of the amounts reaches
+// target_of(their sum); where it does not, all of it.  Its keys lie in low .. high.
+template <class A, class F>
+__device__ __forceinline__ Cut by_logit(Shared &s, int n, int V, uint32_t low, uint32_t high, A amount, F target_of)
+{
+    u64 target = 0;
+    for (bool first = true;; first = false) {
+        const int shift = key_shift(high - low);
+        auto key = [&](int x) { return key_of(s.list.l[x]); };
+        auto in = [&](int x) { return key(x) >= low && key(x) <= high; };
+        clear(s);
+        for (int x = threadIdx.x; x < n; x += NT) {
+            const u64 a = in(x) ? amount(x) : 0;
+            if (a)
+                atomicAdd(&s.bins[(high - key(x)) >> shift], a);
+        }
+        __syncthreads();
+        if (!find(s, [&](u64 all) { return first ? target = target_of(all) : target; }))
+            return Cut{-__builtin_inff(), -1};
+        target -= s.before;
+        narrow(low, high, s.bin, shift);
+        const uint32_t found = pick(s, n, in, amount);
+        if (found <= 64)
+            return rank<false>(s, (int)found, target);
+        if (low == high)
+            return by_number(s, n, V, [&](int x) { return key(x) == low ? amount(x) : 0; },
+                             [&](u64) { return target; });
+    }
+}
+
+// The row's tokens from logit `from` on with in(l, index), in any order, as the list; how
+// many there are (LIST of them are kept).
+template <class T, class In>
+__device__ __forceinline__ uint32_t gather(Shared &s, const Row<T> &row, float from, In in)
+{
+    __syncthreads();
+    if (threadIdx.x == 0)
+        s.found = 0;
+    __syncthreads();
+    row.each_from(from, [&](int t, const float (&l)[8]) {
+        const int lane = threadIdx.x & 63;
+        uint64_t m[8];
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = __ballot(l[e] >= from && in(l[e], row.index(t, e)));
+            n += __builtin_popcountll(m[e]);
+        }
+        int base = 0;
+        if (lane == 0 && n > 0)
+            base = (int)atomicAdd(&s.found, (uint32_t)n);
+        base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (m[e] == 0)
+                continue;
+            const int x = base + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m[e] >> 32),
+                                                                __builtin_amdgcn_mbcnt_lo((uint32_t)m[e], 0));
+            if ((m[e] >> lane & 1) && x < LIST) {
+                s.list.l[x] = l[e];
+                s.list.at[x] = row.index(t, e);
+            }
+            base += __builtin_popcountll(m[e]);
+        }
+    });
+    __syncthreads();
+    return s.found;
+}
+
+// Cuts what is left of a row, by its tokens with keys low .. high, to its beginning (by
+// logit) whose amounts (1, or the weights) reach target, which they do.
+template <bool WEIGHTS, class T>
+__device__ void by_row(Shared &s, const Row<T> &row, const Weights &w, Cut &c, u64 target, uint32_t low, uint32_t high)
+{
+    for (;;) {
+        auto in = [&](float l, int i) { return key_of(l) <= high && c.keeps(l, i); };
+        const float from = of_key(low);
+        const uint32_t n = gather(s, row, from, in);
+        if (n <= LIST) {
+            for (uint32_t x = threadIdx.x; x < n; x += NT)
+                s.list.w[x] = WEIGHTS ? w(s.list.l[x]) : 1;
+            c = by_logit(s, (int)n, row.V, low, high, [&](int x) { return s.list.w[x]; }, [&](u64) { return target; });
+            return;
+        }
+        if (low == high) {  // equal ones: the first in the order of the vocabulary
+            const float l = of_key(low);
+            const u64 each = WEIGHTS ? w(l) : 1;
+            const u64 k = (target + each - 1) / each;
+            const Cut was = c;
+            c.at = nth(s, row, k, [&](float x, int i) { return x == l && was.keeps(x, i); });
+            c.cut = l;
+            return;
+        }
+        const int shift = key_shift(high - low);
+        clear(s);
+        row.each_from(from, [&](int t, const float (&l)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (l[e] >= from && in(l[e], row.index(t, e)))
+                    atomicAdd(&s.bins[(high - key_of(l[e])) >> shift], WEIGHTS ? w(l[e]) : 1);
+        });
+        __syncthreads();
+        find(s, [&](u64) { return target; });
+        target -= s.before;
+        narrow(low, high, s.bin, shift);
+    }
 }
 
 template <class T>
@@ -365,120 +632,234 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
 {
     __shared__ Shared s;
     const int64_t r = blockIdx.x;
-    const Row<T> row(a, r);
+    const Row<T> row(a, r, s);
     const float inf = __builtin_inff();
     float m = -inf;
-    row.each([&](int, const float (&l)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            m = fmaxf(m, l[e]);
-    });
+    row.tops([&](float l) { m = fmaxf(m, l); });
     m = block_max(m, s.sums);
     if (m == -inf) {  // nothing is left to choose
         if (threadIdx.x == 0)
             a.tokens[r] = -1;
         return;
     }
-    const float temp = a.temperature ? a.temperature[r] : 1.0f;
+    const float temp = a.temperature ? std::min(a.temperature[r], MOST) : 1.0f;
     if (!(temp > 0.0f)) {
-        const int at = nth(s, row, 1, [&](float l, int) { return l == m; });
         if (threadIdx.x == 0)
-            a.tokens[r] = at;
+            s.token = a.V;
+        __syncthreads();
+        int first = a.V;
+        row.each_from(m, [&](int t, const float (&l)[8]) {
+#pragma unroll
+            for (int e = 7; e >= 0; --e)
+                first = l[e] == m ? std::min(first, row.index(t, e)) : first;
+        });
+        if (first < a.V)
+            atomicMin(&s.token, first);
+        __syncthreads();
+        if (threadIdx.x == 0)
+            a.tokens[r] = s.token;
         return;
     }
-    if (threadIdx.x < 64) {  // the series of exp, up to 2^-60 of it
-        const double x = threadIdx.x * (0.693147180559945309417 / 64.0);
+    if (threadIdx.x < STEPS) {  // the series of exp, up to 2^-60 of it
+        const double x = threadIdx.x * (0.693147180559945309417 / STEPS);
         double p = 1.0;
+#pragma unroll
         for (int i = 18; i > 0; --i)
-            p = __builtin_fma(p, x / i, 1.0);
-        s.pow2[threadIdx.x] = p;
+            p = __builtin_fma(p * x, 1.0 / i, 1.0);
+        s.pow2[threadIdx.x] = __builtin_ldexp(p, a.log2_one);
     }
     Weights w;
-    w.m = m;
-    w.step = 64.0 * 1.44269504088896340736 / (double)temp;
-    w.one = a.log2_one;
+    w.m = std::min(m, MOST);
+    w.step = STEPS * 1.44269504088896340736 / (double)temp;
     w.bin = (float)(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp);
     w.pow2 = s.pow2;
+    __syncthreads();
 
+    int k = a.top_k ? a.top_k[r] : 0;
+    k = k < a.V ? std::max(k, 0) : 0;
+    float p = a.top_p ? a.top_p[r] : 1.0f;
+    p = p < 1.0f ? p : 1.0f;
+    const float mp = a.min_p ? a.min_p[r] : 0.0f;
+    float least = -MOST;
+    if (mp > 0.0f) {  // (not a number: none)
+        const double from = std::min((double)mp, 1.0) * w.pow2[0];
+        least = least_logit(s, m, [&](float l) { return w.real(l) >= from; });
+    }
+    const float u = a.u[r];
+    // What is left: by the cut, and once it is few, the list (n tokens with keys low .. high).
     Cut c = {-inf, -1};
-    const int k = a.top_k ? a.top_k[r] : 0;
-    if (k > 0 && k < a.V) {
-        clear(s);
-        row.each([&](int, const float (&l)[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int b = w.bin_of(l[e]);
+    bool listed = false;
+    uint32_t n = 0, low = 0, high = 0;
+    auto gathered = [&](float from) {
+        with_cut(c, [&](auto exact) {
+            n = gather(s, row, from, [&](float l, int i) { return !exact || c.keeps(l, i); });
+        });
+        low = key_of(from);
+        high = key_of(m);
+        listed = n <= LIST;
+        if (listed)
+            for (uint32_t x = threadIdx.x; x < n; x += NT)
+                s.list.w[x] = w(s.list.l[x]);
+    };
+    auto weight = [&](int x) { return c.keeps(s.list.l[x], s.list.at[x]) ? s.list.w[x] : 0; };
+    if (k > 0) {
+        if (k <= LIST) {
+            clear(s);
+            row.tops([&](float l) {
+                const int b = w.bin_of(l);
                 if (b < BINS)
-                    atomicAdd(&s.count[b], 1u);
+                    atomicAdd(&s.bins[b], 1ull);
+            });
+            __syncthreads();
+            const int b = find(s, [&](u64) { return (u64)k; }) ? (int)s.bin : BINS - 1;
+            // (all of bin b, and a little of the next: the bin's own rounding is 2^-12 of one)
+            gathered(fmaxf(w.m - ((float)b + 1.01f) / w.bin, -MOST));
+        }
+        if (listed) {
+            if (k < (int)n)
+                c = by_logit(s, (int)n, row.V, low, high, [](int) { return (u64)1; }, [&](u64) { return (u64)k; });
+        } else {
+            clear(s);
+            row.each([&](int, const float (&l)[8]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int b = w.bin_of(l[e]);
+                    if (b < BINS)
+                        atomicAdd(&s.bins[b], 1ull);
+                }
+            });
+            __syncthreads();
+            if (find(s, [&](u64) { return (u64)k; })) {
+                const int b = (int)s.bin;
+                const u64 before = s.before;
+                const float from = least_logit(s, m, [&](float l) { return w.bin_of(l) <= b; });
+                const float to = b ? least_logit(s, m, [&](float l) { return w.bin_of(l) < b; }) : inf;
+                by_row<false>(s, row, w, c, k - before, key_of(from), b ? key_of(to) - 1 : key_of(m));
             }
+        }
+    }
+    if (p < 1.0f && listed) {
+        c = by_logit(s, (int)n, row.V, low, high, weight, [&](u64 all) { return share_of(p, all); });
+    } else if (p < 1.0f) {
+        clear(s);
+        with_cut(c, [&](auto exact) {
+            row.each([&](int t, const float (&l)[8]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    int step;
+                    u64 x = w.whole(l[e], step);
+                    if (exact)
+                        x &= c.keeps(l[e], row.index(t, e)) ? ~0ull : 0;
+                    if (x)
+                        atomicAdd(&s.bins[w.bin_of_step(step)], x);
+                }
+            });
         });
         __syncthreads();
-        cut_to<false>(s, row, w, c, (u64)k);
+        u64 target = 0;
+        find(s, [&](u64 all) { return target = share_of(p, all); });
+        const int b = (int)s.bin;
+        const u64 before = s.before;
+        const float from = least_logit(s, m, [&](float l) { return w.weight_bin(l) <= b; });
+        gathered(from);
+        if (listed) {
+            c = by_logit(s, (int)n, row.V, low, high, weight, [&](u64) { return target; });
+        } else {
+            const float to = b ? least_logit(s, m, [&](float l) { return w.weight_bin(l) < b; }) : inf;
+            by_row<true>(s, row, w, c, target - before, key_of(from), b ? key_of(to) - 1 : key_of(m));
+        }
+    } else if (!listed && least > -MOST) {
+        gathered(least);
     }
-    const float p = a.top_p ? a.top_p[r] : 1.0f;
-    if (p < 1.0f) {
-        clear(s);
-        u64 sum = 0, all;
-        row.each([&](int t, const float (&l)[8]) {
+    if (listed) {
+        c = by_number(s, (int)n, row.V, [&](int x) { return s.list.l[x] < least ? 0 : weight(x); },
+                      [&](u64 all) { return draw(u, all) + 1; });
+        if (threadIdx.x == 0)
+            a.tokens[r] = c.at;
+        return;
+    }
+
+    // What is left, by sixteenths of the row, a wave each.  Where it is few of a tile's
+    // tokens they are gathered in LDS, 64 to be weighed at once.
+    if (c.cut < least && least > -MOST)
+        c = Cut{of_key(key_of(least) - 1), -1};
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (row.tiles + WAVES - 1) / WAVES;
+    __syncthreads();
+    float *few = reinterpret_cast<float *>(&s.list) + wave * ((int)sizeof(s.list) / WAVES / 4);
+    static_assert(sizeof(s.list) / WAVES / 4 >= TILE + 64, "a tile's tokens and what an earlier one left");
+    int held = 0;
+    u64 mine = 0;
+    with_cut(c, [&](auto exact) {
+        row.each(wave * per, std::min(row.tiles, (wave + 1) * per), 1, [&](int t, const float (&l)[8]) {
+            uint64_t m[8];
+            int n = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int b = w.bin_of(l[e]);
-                if (b < BINS && c.keeps(l[e], row.index(t, e))) {
-                    const u64 x = w(l[e]);
-                    atomicAdd(&s.count[b], 1u);
-                    atomicAdd(&s.weight[b], x);
-                    sum += x;
-                }
+                m[e] = __ballot(c.keeps<decltype(exact)::value>(l[e], row.index(t, e)));
+                n += __builtin_popcountll(m[e]);
             }
+            if (n > TILE / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    mine += w(l[e]) & (m[e] >> lane & 1 ? ~0ull : 0);
+                return;
+            }
+            if (n == 0)
+                return;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (m[e] >> lane & 1)
+                    few[held + __builtin_popcountll(m[e] & ((1ull << lane) - 1))] = l[e];
+                held += __builtin_popcountll(m[e]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (; held >= 64; held -= 64)
+                mine += w(few[held - 64 + lane]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         });
-        block_scan<WAVES>(sum, s.sums, all);
-        const double t = __builtin_ceil((double)p * (double)all);
-        cut_to<true>(s, row, w, c, t < 1.0 ? 1 : std::min((u64)t, all));
-    }
-    const double least = a.min_p ? std::min((double)a.min_p[r], 1.0) : 0.0;  // (NaN: none)
-    auto left = [&](float l, int i) -> u64 {
-        if (!(l > -inf) || !c.keeps(l, i))
-            return 0;
-        const double x = w.real(l);
-        return x < least ? 0 : w.whole(x);
-    };
+    });
+    if (lane < held)
+        mine += w(few[lane]);
+    mine = wave_scan(mine);
+    if (lane == 63)
+        s.tile[wave] = mine;
     __syncthreads();
-    row.each([&](int t, const float (&l)[8]) {
+    u64 all = 0, before = 0;
+    for (int x = 0; x < WAVES; ++x)
+        all += s.tile[x];
+    const u64 target = draw(u, all);
+    int part = 0;
+    for (int x = 0; x < WAVES; ++x) {
+        const u64 n = s.tile[x];
+        if (before + n > target) {
+            part = x;
+            break;
+        }
+        before += n;
+    }
+    __syncthreads();
+    // its tiles, and the tile's tokens
+    const int first = part * per, end = std::min(row.tiles, first + per);
+    row.each(first + wave, end, WAVES, [&](int t, const float (&l)[8]) {
         u64 sum = 0;
-        bool any = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            any |= c.keeps(l[e], row.index(t, e));
-        if (__any(any)) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                sum += left(l[e], row.index(t, e));
-            for (int d = 1; d < 64; d <<= 1)
-                sum += __shfl_xor(sum, d);
-        }
-        if ((threadIdx.x & 63) == 0)
+            sum += w(l[e]) & (c.keeps(l[e], row.index(t, e)) ? ~0ull : 0);
+        sum = wave_scan(sum);
+        if (lane == 63)
             s.tile[t] = sum;
     });
     __syncthreads();
-    u64 total = 0;
-    for (int t = threadIdx.x; t < row.tiles; t += NT)
-        total += s.tile[t];
-    u64 all;
-    block_scan<WAVES>(total, s.sums, all);
-    const float u = a.u[r];
-    const double share = u > 0.0f ? std::min((double)u, 1.0) * (double)all : 0.0;
-    const u64 target = std::min((u64)share, all - 1);  // the first whose sum is above it
-    u64 before = 0;
-    for (int t0 = 0; t0 < row.tiles; t0 += NT) {
-        const int t = t0 + threadIdx.x;
-        const u64 n = t < row.tiles ? s.tile[t] : 0;
-        u64 step;
-        const u64 b = before + block_scan<WAVES>(n, s.sums, step);
+    {
+        static_assert(TILES / WAVES < NT, "a thread for each");
+        const int t = first + threadIdx.x;
+        const u64 n = t < end ? s.tile[t] : 0;
+        u64 ignore;
+        const u64 b = before + block_scan<WAVES>(n, s.sums, ignore);
         if (b <= target && target < b + n) {
             s.bin = t;
             s.before = b;
         }
-        before += step;
     }
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -488,15 +869,10 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
         u64 x[8], sum = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            x[e] = left(l[e], row.index(t, e));
+            x[e] = w(l[e]) & (c.keeps(l[e], row.index(t, e)) ? ~0ull : 0);
             sum += x[e];
         }
-        u64 upto = sum;
-        for (int d = 1; d < 64; d <<= 1) {
-            const u64 y = __shfl_up(upto, d);
-            upto += (int)threadIdx.x >= d ? y : 0;
-        }
-        u64 at = s.before + upto - sum;
+        u64 at = s.before + wave_scan(sum) - sum;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (at <= target && target < at + x[e])

@@ -12,7 +12,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     out = []
     for r in range(rows):
         x = logits[r].astype(np.float64)
-        x = np.where(np.isnan(x), -np.inf, x)
+        x = np.minimum(np.where(np.isnan(x), -np.inf, x), float(np.finfo(np.float32).max))
         m = x.max()
         if m == -np.inf:
             out.append(-1)
@@ -28,11 +28,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
         if k > 0:
             order = order[:k]
         with np.errstate(invalid="ignore", over="ignore"):
-            away = np.where(x == m, 0.0, (x - m) / t if t < np.inf or m < np.inf else -np.inf)
-            w = np.exp(away)
-        w = np.where(x == -np.inf, 0.0, w)
-        if m == np.inf:
-            w = (x == m).astype(np.float64)
+            w = np.exp(np.where(x > -np.inf, (x - m) / t, -np.inf))
         whole = np.rint(w * 2.0 ** one_of(V)).astype(np.int64)  # below 2^52 each
         p = 1.0 if top_p is None else float(top_p[r])
         if p < 1:
