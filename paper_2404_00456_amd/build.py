@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libquarot.so")
 SOURCES = ["capi.cpp", "host_rules.cpp", "rotate_quant.hip", "gemm_w4a4.hip", "gemm_stream.hip",
            "gemm_mid.hip", "gemm_grouped.hip", "kv_attention.hip", "scratch.hip",
            "capi_paged.cpp", "paged_append.hip", "paged_attention.hip",
-           "capi_scored.cpp", "paged_scored.hip", "capi_pages.cpp", "pages.hip",
+           "capi_scored.cpp", "paged_scored.hip", "paged_scored_large.hip", "capi_pages.cpp", "pages.hip",
            "capi_sample.cpp", "sample.hip"]
 # MFMA-only rate probes and the device's peak clock (include/quarot_probe.h)
 PROBE_LIB = os.path.join(HERE, "libquarot_probe.so")

@@ -41,6 +41,18 @@ __device__ __forceinline__ T lane_value(T v, int lane)
         return (T)lo;
 }
 
+// The largest v >= 0 of a wave.
+__device__ __forceinline__ int wave_max(int v)
+{
+    v = max(v, lane_before<0x111, 0xF>(v));
+    v = max(v, lane_before<0x112, 0xF>(v));
+    v = max(v, lane_before<0x114, 0xF>(v));
+    v = max(v, lane_before<0x118, 0xF>(v));
+    v = max(v, lane_before<0x142, 0xA>(v));
+    v = max(v, lane_before<0x143, 0xC>(v));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 // The sum of v over the threads before this one; `all` the sum of all.  `sums` holds one
 // value a wave (16 at most); every thread of the block calls it.  (By shuffles and a loop
 // over the waves' sums it took half a microsecond in 64 bits.)

@@ -114,5 +114,6 @@ __device__ __forceinline__ void search(const PagedMap &m, int &lo, int &n, Befor
 hipError_t launch_append(const AppendArgs &a, hipStream_t s);
 hipError_t launch_paged_attention(const PagedAttnArgs &a, int rows, hipStream_t s);
 hipError_t launch_scored_attention(const ScoredAttnArgs &a, int rows, hipStream_t s);
+hipError_t launch_large_cap_attention(const ScoredAttnArgs &a, int rows, hipStream_t s);
 
 }  // namespace quarot

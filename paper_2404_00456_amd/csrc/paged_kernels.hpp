@@ -37,6 +37,7 @@
 
 #include <algorithm>
 
+#include "block_scan.hpp"
 #include "lds_dma.hpp"
 #include "paged.hpp"
 
@@ -59,7 +60,7 @@ constexpr float TOP_TILE = 6.0f, TOP_ROWS = 8.0f;
 
 // Forms of the kernels.
 struct Plain {
-    static constexpr bool SCORED = false, CAP = false, BIAS = false;
+    static constexpr bool SCORED = false, CAP = false, LARGE = false, BIAS = false;
     using Args = PagedAttnArgs;
 };
 
@@ -69,9 +70,16 @@ struct Plain {
 // d is the distance of the nearest token that the query sees: a constant of its row,
 // which no softmax changes, and without which a query that sees only far tokens would
 // take its weights from the last bits of large numbers.
-template <bool CAP_, bool BIAS_>
+// c - 2 c / (1 + e) is off by some 2^-23 c, whatever the score is: 2e-5 log2 units for a
+// cap of 128.  Caps beyond CAP_LARGE are forms of their own, which take scores below an
+// eighth of them by the series of tanh instead (its next term is 1.3e-9 of the score there).
+constexpr float CAP_LARGE = 128.0f;
+
+enum Cap { NO_CAP, CAP, LARGE_CAP };
+
+template <Cap CAP_, bool BIAS_>
 struct Scored {
-    static constexpr bool SCORED = true, CAP = CAP_, BIAS = BIAS_;
+    static constexpr bool SCORED = true, CAP = CAP_ != NO_CAP, LARGE = CAP_ == LARGE_CAP, BIAS = BIAS_;
     using Args = ScoredAttnArgs;
 };
 
@@ -126,32 +134,36 @@ __device__ __forceinline__ bool sees(const View &v, int t, int sinks)
     return (t < v.high) & ((t >= v.low) | (t < sinks));
 }
 
-// c - 2 c / (1 + e) is off by some 2^-23 c, whatever the score is: 2e-5 log2 units for a
-// cap of 128.  Caps beyond that take scores below an eighth of them by the series of tanh
-// instead (its next term is 1.3e-9 of the score there).
-constexpr float CAP_LARGE = 128.0f;
+// A score in log2 units, capped.
+template <class M>
+__device__ __forceinline__ float capped(const typename M::Args &a, float x)
+{
+    if constexpr (M::CAP) {
+        const float c = a.cap * LOG2E;
+        const float e = __builtin_amdgcn_exp2f(x * (2.0f / a.cap));
+        float z = __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(e + 1.0f), c);
+        if constexpr (M::LARGE) {
+            const float y = x / c, t = y * y;
+            const float f = __builtin_fmaf(
+                t, __builtin_fmaf(t, __builtin_fmaf(t, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+            z = fabsf(y) < 0.125f ? x * f : z;
+        }
+        return z;
+    }
+    return x;
+}
 
-// A score in log2 units as the form has it.
+// What a capped score loses by its token's distance.
+template <class M>
+__device__ __forceinline__ float fallen(const View &v, float x, int t)
+{
+    return M::BIAS ? __builtin_fmaf(-v.slope, (float)(abs(v.p - t) - v.near), x) : x;
+}
+
 template <class M>
 __device__ __forceinline__ float shaped(const typename M::Args &a, const View &v, float x, int t)
 {
-    if constexpr (M::CAP) {
-        if (a.cap > 0.0f) {
-            const float c = a.cap * LOG2E;
-            const float e = __builtin_amdgcn_exp2f(x * (2.0f / a.cap));
-            float z = __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(e + 1.0f), c);
-            if (a.cap > CAP_LARGE) {
-                const float y = x / c, t = y * y;
-                const float f = __builtin_fmaf(
-                    t, __builtin_fmaf(t, __builtin_fmaf(t, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-                z = fabsf(y) < 0.125f ? x * f : z;
-            }
-            x = z;
-        }
-    }
-    if constexpr (M::BIAS)
-        x = __builtin_fmaf(-v.slope, (float)(abs(v.p - t) - v.near), x);
-    return x;
+    return fallen<M>(v, capped<M>(a, x), t);
 }
 
 // The tokens that a block's rows see, from those of its new tokens (each wave for
@@ -169,17 +181,14 @@ __device__ __forceinline__ void reach(const typename M::Args &a, Work &w, int mr
         high = max(high, v.high);
         every = min(every, v.high);
     }
-    if (k0 != k1)
-        for (int d = 1; d < 64; d <<= 1) {
-            low = min(low, __shfl_xor(low, d));
-            after = max(after, __shfl_xor(after, d));
-            high = max(high, __shfl_xor(high, d));
-            every = min(every, __shfl_xor(every, d));
-        }
-    w.every = __builtin_amdgcn_readfirstlane(every) - 1;
-    w.after = __builtin_amdgcn_readfirstlane(after) - 1;
-    paged::cut(w, __builtin_amdgcn_readfirstlane(low), __builtin_amdgcn_readfirstlane(high),
-               a.map.max_pages * a.map.page, a.sinks, a.splits, a.least);
+    const int most = 0x7FFFFFFF;  // (a least one as what the largest complement leaves)
+    high = wave_max(high);
+    after = wave_max(after);
+    low = most - wave_max(most - low);
+    every = most - wave_max(most - every);
+    w.every = every - 1;
+    w.after = after - 1;
+    paged::cut(w, low, high, a.map.max_pages * a.map.page, a.sinks, a.splits, a.least);
 }
 
 template <class M>
@@ -790,9 +799,11 @@ __global__ __launch_bounds__(64 * NW)
 
     // Scores with a form: where no row's tokens of a round lie on both sides of it, a
     // register's distance is a multiple of the slope away from that of the round's first,
-    // so that the distance costs one instruction a score and the cap four.  Rounds that
-    // hold a row's own position, or tokens that some row does not see, go through settle's
-    // exact way (hidden: a bit for each register).
+    // so that the distance costs one instruction a score and the cap four.  A cap's come a
+    // part of the round before the rest (ready: a score becomes 1 / (1 + e), since one
+    // after the other its exponential, reciprocal and weight wait for each other).  Rounds
+    // that hold a row's own position, or tokens that some row does not see, go through
+    // settle's exact way (hidden: a bit for each register).
     constexpr bool FORM = M::CAP || M::BIAS;
     struct Form {
         float base, slope;
@@ -800,15 +811,21 @@ __global__ __launch_bounds__(64 * NW)
         uint32_t hidden;
         bool exact;
     };
-    float top = 0.0f, ck = 0.0f;
+    // a ready score times `times` plus `top` is a score
+    float top = 0.0f, times = c2, ck = 0.0f;
     if constexpr (M::CAP) {
-        top = a.cap * LOG2E;
+        top = M::LARGE ? 0.0f : a.cap * LOG2E;
+        times = M::LARGE ? 1.0f : -2.0f * top;
         ck = c2 * (2.0f / a.cap);
     }
+    auto ready = [&](v16f &s, int r) {
+        if constexpr (M::LARGE)
+            s[r] = capped<M>(a, s[r] * c2);
+        else if constexpr (M::CAP)
+            s[r] = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * ck) + 1.0f);
+    };
     auto form = [&](int t0, uint32_t hidden, bool edge) {
         Form f = {top, 0.0f, t0 + 4 * hf, hidden, edge};
-        if constexpr (M::CAP)
-            f.exact |= a.cap > CAP_LARGE;
         if constexpr (M::BIAS) {
             const bool behind = t0 >= pmax;  // (of the block: the same for all its waves)
             f.exact |= !behind && t0 + 31 > pmin;
@@ -823,11 +840,7 @@ __global__ __launch_bounds__(64 * NW)
             x = f.base - ms;
             if constexpr (M::BIAS)
                 x = __builtin_fmaf(f.slope, (float)(8 * (r >> 2) + (r & 3)), x);
-            if constexpr (M::CAP)
-                x = __builtin_fmaf(-2.0f * top,
-                                   __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * ck) + 1.0f), x);
-            else
-                x = __builtin_fmaf(s[r], c2, x);
+            x = __builtin_fmaf(s[r], times, x);
         } else {
             x = __builtin_fmaf(s[r], c2, -ms);
         }
@@ -859,7 +872,7 @@ __global__ __launch_bounds__(64 * NW)
             if constexpr (FORM) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float x = shaped<M>(a, vw, s[r] * c2, f0.t0 + 8 * (r >> 2) + (r & 3));
+                    const float x = fallen<M>(vw, __builtin_fmaf(s[r], times, top), f0.t0 + 8 * (r >> 2) + (r & 3));
                     s[r] = f0.hidden >> r & 1 ? -inf : x;
                 }
             }
@@ -923,6 +936,11 @@ __global__ __launch_bounds__(64 * NW)
             kf[c] = kfrag(c);
             vf[c] = vfrag(c);
         }
+        constexpr int SOON = KS == 4 ? 4 : 2;  // a part's scores
+        if constexpr (M::CAP)
+#pragma unroll
+            for (int r = 0; r < SOON; ++r)
+                ready(sc, r);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < KS; ++c) {
@@ -933,6 +951,10 @@ __global__ __launch_bounds__(64 * NW)
             for (int r = 16 * c / KS; r < 16 * (c + 1) / KS; r += 2) {
                 if (KS == 16 && (c & 1))
                     continue;  // a part's share is one weight: two with every other
+                if (M::CAP && r + SOON < 16) {
+                    ready(sc, r + SOON);
+                    ready(sc, r + SOON + 1);
+                }
                 ls[0] += weight(sc, pb, ms, r, f);
                 ls[1] += weight(sc, pb, ms, r + 1, f);
             }
@@ -951,9 +973,11 @@ __global__ __launch_bounds__(64 * NW)
         constexpr int H = 64 / TS;      // stages of a step
         constexpr int PM = Sh::PAIRS / KS;  // pairs with a part
         const NibConst nk = nib_const();
-        // first token of stage j; past the last one, the last one again
+        // first token of stage j; past the last one, the last one again.  Where scores fall
+        // by distance the nearest come first: from far to near, a steep slope moved the
+        // reference in every round (a prompt of 8192, 2351 us).
         auto token0 = [&](int j) {
-            const int k = min(j, (end - begin) * H - 1);
+            const int last = (end - begin) * H - 1, k = M::BIAS ? max(last - j, 0) : min(j, last);
             return paged::step_token(w, begin + k / H) + k % H * TS;
         };
         spoiled[wave] = 0;
@@ -1229,7 +1253,22 @@ __global__ __launch_bounds__(64 * ROWS_W)
     const int every = M::SCORED ? w.every : pmin;
     const int after = M::SCORED ? w.after : a.window > 0 ? pmax - a.window : -1;
     const int wfirst = a.window > 0 ? p - a.window : -1;
-    const View vw = view<M>(a, w, w.tok0 + qi, p, pl.h * a.rep + (row - qi * a.rep));
+    // A scored query's view, worked out again where it is looked at (few stages): kept in
+    // registers it made others spill, and a reload waits for all loads on their way (64
+    // sequences of 1 .. 8192 tokens with slopes: 93 us).
+    auto viewed = [&]() {
+        int m = n;
+        asm volatile("" : "+v"(m));
+        const int r = w.row0 + min(m, R - 1), i = r / a.rep;
+        return view<M>(a, w, w.tok0 + i, w.pos0 + i, pl.h * a.rep + (r - i * a.rep));
+    };
+    float fall = 0.0f;  // of a score, for each position before the nearest that is seen
+    int nearest = 0;
+    if constexpr (M::BIAS) {
+        const View v = viewed();
+        fall = v.slope;
+        nearest = v.p - v.near;
+    }
     uint4 qraw[KW];
     {
         const uint16_t *qr = a.q + (int64_t)(w.tok0 + qi) * a.q_stride +
@@ -1242,6 +1281,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
     const int begin = pl.split * w.per + wave, end = min(w.steps, pl.split * w.per + w.per);
     const int stages = begin < end ? 2 * ((end - begin + ROWS_W - 1) / ROWS_W) : 0;
     auto token_at = [&](int k) {
+        k = M::BIAS ? stages - 1 - k : k;  // the nearest first, as in the tiles
         return paged::step_token(w, begin + (k >> 1) * ROWS_W) + 32 * (k & 1);
     };
     uint8_t *ring = lds + wave * (ROWS_NS * Ring::STAGE);
@@ -1368,7 +1408,28 @@ __global__ __launch_bounds__(64 * ROWS_W)
             f[3] = hi[1];
         };
         const float ms = m > -inf ? m : 0.0f;  // nothing seen so far: weights 0
-        const float ms0 = M::SCORED ? 0.0f : -ms;  // (taken off once they have their form)
+        // What is added to a score of token 4 g + r of group u (plus what comes off): the
+        // reference, and with slopes the distance, which is a multiple of the slope away
+        // from that of the stage's first token.  A cap comes in between, and stages with
+        // tokens behind some row's own position take the exact way.
+        constexpr bool FORM = M::CAP || M::BIAS;
+        bool exact = false;
+        float off = -ms, slope = 0.0f;
+        if constexpr (M::CAP) {
+            exact = M::LARGE;
+            off += a.cap * LOG2E;
+        }
+        if constexpr (M::BIAS) {
+            exact |= th + 31 > pmin;
+            slope = fall;
+            off = __builtin_fmaf(slope, (float)(th + 4 * g - nearest), off);
+        }
+        if (FORM && exact)
+            off = slope = 0.0f;
+        auto added = [&](int u, int r) {
+            return M::BIAS ? __builtin_fmaf(slope, (float)(16 * u + r), off) : off;
+        };
+        auto added_first = [&](int u, int r) { return M::CAP ? 0.0f : added(u, r); };
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             uint32_t kc[KW];
@@ -1407,7 +1468,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    x[u][r] = __builtin_fmaf(acc[r], c2, ms0);
+                    x[u][r] = __builtin_fmaf(acc[r], c2, added_first(u, r));
                 continue;
             }
             v4f acc = {q64, q64, q64, q64};
@@ -1426,19 +1487,31 @@ __global__ __launch_bounds__(64 * ROWS_W)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 x[u][r] = __builtin_fmaf((float)ksh[u][r], acc[r] * c2,
-                                         __builtin_fmaf((float)kzh[u][r], qs, ms0));
+                                         __builtin_fmaf((float)kzh[u][r], qs, added_first(u, r)));
         }
-        if constexpr (M::SCORED) {
+        if (FORM && exact) {
+            const View vw = viewed();
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     x[u][r] = shaped<M>(a, vw, x[u][r], th + 16 * u + 4 * g + r) - ms;
+        } else if constexpr (M::CAP) {
+            const float top2 = -2.0f * LOG2E * a.cap, rate = 2.0f / a.cap;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[u][r] = __builtin_fmaf(
+                        top2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[u][r] * rate) + 1.0f), added(u, r));
         }
         const bool edge = ok != 3 || th + 31 > every ||
                           (M::SCORED ? th <= after : a.window > 0 && th <= pmax - a.window);
         if (edge) {
             asm volatile("");  // a branch, not selects in every step
+            View vw = {};
+            if constexpr (M::SCORED)
+                vw = viewed();
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -1737,15 +1810,14 @@ __global__ __launch_bounds__(256) void k_paged_combine(typename M::Args a)
     }
 }
 
-// The few-row kernel and the joining take every scored form at run time (they wait for
-// memory), the tiles have one kernel for each.
+// The joining needs no more of a form than that it is one.
 template <class M>
 struct Any {
     using T = M;
 };
-template <bool CAP, bool BIAS>
-struct Any<Scored<CAP, BIAS>> {
-    using T = Scored<true, true>;
+template <Cap C, bool BIAS>
+struct Any<Scored<C, BIAS>> {
+    using T = Scored<NO_CAP, false>;
 };
 
 template <int D, int MR, class M>
@@ -1797,14 +1869,14 @@ hipError_t go_few(const typename M::Args &a, hipStream_t s)
         break;
     }
     hipError_t e = hipGetLastError();
-    return e != hipSuccess || a.splits == 1 ? e : go_combine<D, MR, M>(a, slots, s);
+    return e != hipSuccess || a.splits == 1 ? e : go_combine<D, MR, typename Any<M>::T>(a, slots, s);
 }
 
 template <int D, class M>
 hipError_t go_rows(const typename M::Args &a, int rows, hipStream_t s)
 {
     if (rows == paged::FEW_ROWS)
-        return go_few<D, typename Any<M>::T>(a, s);
+        return go_few<D, M>(a, s);
     if constexpr (D < 256) {
         if (rows == 64)
             return go_tile<D, 2, M>(a, s);
