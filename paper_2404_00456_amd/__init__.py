@@ -1192,21 +1192,29 @@ def quarot_kv_paged_attention_scored(q: torch.Tensor, k_cache, v_cache, page_tab
                             n_sinks, max_seq_len, sm_scale, out, workspace, stream, scoring)
 
 
-def _pages(page_table, page_refs, seq_lens=None, **more):
-    """Sequences, entries of each and pages; the addresses of the table, the lengths, the
-    references and `more` (name: (int32 tensor, length))."""
+def _ints(dev, *named):
+    """Addresses of int32 tensors (tensor, length or None, name) on `dev`: looked at in one
+    go where all is as it should be, as in nearly every call."""
+    i32, at = torch.int32, []
+    for t, n, name in named:
+        if not isinstance(t, torch.Tensor) or t.dtype != i32 or t.device != dev or \
+                not t.is_contiguous() or not t.is_cuda or (n is not None and t.shape != (n,)):
+            _ptr(t, i32, name)
+            if n is not None:
+                _shape(t, (n,), name)
+            _on_device(dev, **{name: t})
+        at.append(t.data_ptr())
+    return at
+
+
+def _pages(page_table, page_refs, stream):
+    """Device, sequences, entries of each and pages."""
     _ndim(page_table, 2, "page_table")
     _ndim(page_refs, 1, "page_refs")
     B, P = page_table.shape
-    at = [_ptr(page_table, torch.int32, "page_table")]
-    if seq_lens is not None:
-        _shape(seq_lens, (B,), "seq_lens")
-        at.append(_ptr(seq_lens, torch.int32, "seq_lens"))
-    at.append(_ptr(page_refs, torch.int32, "page_refs"))
-    for name, (t, n) in more.items():
-        _shape(t, (n,), name)
-        at.append(_ptr(t, torch.int32, name))
-    return at, B, P, page_refs.shape[0]
+    dev = page_table.device
+    _on_device(dev, stream)
+    return dev, B, P, page_refs.shape[0]
 
 
 def quarot_kv_pages_workspace_size(n_pages: int) -> int:
@@ -1216,7 +1224,9 @@ def quarot_kv_pages_workspace_size(n_pages: int) -> int:
 
 def _pages_workspace(workspace, n: int, dev, stream):
     if workspace is None:
-        workspace = _new((quarot_kv_pages_workspace_size(n),), torch.uint8, dev, stream)
+        workspace = _new((lib().quarot_kv_pages_workspace_size(n),), torch.uint8, dev, stream)
+    else:
+        _on_device(dev, workspace=workspace)
     return workspace, _ptr(workspace, torch.uint8, "workspace"), workspace.numel()
 
 
@@ -1227,8 +1237,9 @@ def quarot_kv_pages_fork(page_table: torch.Tensor, seq_lens: torch.Tensor, page_
     row of page_table int32 [batch, max_pages] and its length become those, its pages are
     shared; with a parent that is no sequence (-1) it ends.  page_refs int32 [n_pages]
     counts the entries that hold a page (0: free)."""
-    at, B, P, n = _pages(page_table, page_refs, seq_lens, parent=(parent, page_table.shape[0]))
-    _on_device(page_table.device, stream, seq_lens=seq_lens, page_refs=page_refs, parent=parent)
+    dev, B, P, n = _pages(page_table, page_refs, stream)
+    at = _ints(dev, (page_table, None, "page_table"), (seq_lens, B, "seq_lens"),
+               (page_refs, None, "page_refs"), (parent, B, "parent"))
     _check("quarot_kv_pages_fork", lib().quarot_kv_pages_fork(*at, B, P, n, _stream(stream)))
 
 
@@ -1245,17 +1256,21 @@ def quarot_kv_pages_reserve(page_table: torch.Tensor, seq_lens: torch.Tensor,
     rows for the append and the attention, the pages to copy in every layer's pools first
     (quarot_kv_pages_copy; -1: none), and 0, or the pages that were lacking (-1: positions),
     where nothing has changed and cu_new is 0."""
-    B, dev = page_table.shape[0], page_table.device
-    out = [_new((m,), torch.int32, dev, stream) if t is None else t
-           for t, m in ((cu_new, B + 1), (copy_src, B), (copy_dst, B), (missing, 1))]
-    at, B, P, n = _pages(page_table, page_refs, seq_lens, n_new=(n_new, B), cu_new=(out[0], B + 1),
-                         copy_src=(out[1], B), copy_dst=(out[2], B), missing=(out[3], 1))
-    _on_device(dev, stream, seq_lens=seq_lens, page_refs=page_refs, n_new=n_new, cu_new=out[0],
-               copy_src=out[1], copy_dst=out[2], missing=out[3], workspace=workspace)
+    dev, B, P, n = _pages(page_table, page_refs, stream)
+    if cu_new is None and copy_src is None and copy_dst is None and missing is None:
+        cu_new, copy_src, copy_dst, missing = \
+            _new((3 * B + 2,), torch.int32, dev, stream).split((B + 1, B, B, 1))
+    else:
+        cu_new, copy_src, copy_dst, missing = (
+            _new((m,), torch.int32, dev, stream) if t is None else t
+            for t, m in ((cu_new, B + 1), (copy_src, B), (copy_dst, B), (missing, 1)))
+    at = _ints(dev, (page_table, None, "page_table"), (seq_lens, B, "seq_lens"),
+               (page_refs, None, "page_refs"), (n_new, B, "n_new"), (cu_new, B + 1, "cu_new"),
+               (copy_src, B, "copy_src"), (copy_dst, B, "copy_dst"), (missing, 1, "missing"))
     workspace, ws, size = _pages_workspace(workspace, n, dev, stream)
     _check("quarot_kv_pages_reserve", lib().quarot_kv_pages_reserve(
         *at, B, P, n, int(page_size), ws, size, _stream(stream)))
-    return tuple(out)
+    return cu_new, copy_src, copy_dst, missing
 
 
 def quarot_kv_pages_compact(page_table: torch.Tensor, page_refs: torch.Tensor,
@@ -1267,17 +1282,19 @@ def quarot_kv_pages_compact(page_table: torch.Tensor, page_refs: torch.Tensor,
     """The pages that are held get the lowest numbers, in place.  Returns (move_src,
     move_dst, n_live): the pages to copy in every layer's pools (int32 [n_pages / 2], -1
     behind the last), and how many are held."""
-    dev, n = page_table.device, page_refs.shape[0]
-    out = [_new((m,), torch.int32, dev, stream) if t is None else t
-           for t, m in ((move_src, n // 2), (move_dst, n // 2), (n_live, 1))]
-    at, B, P, n = _pages(page_table, page_refs, move_src=(out[0], n // 2), move_dst=(out[1], n // 2),
-                         n_live=(out[2], 1))
-    _on_device(dev, stream, page_refs=page_refs, move_src=out[0], move_dst=out[1], n_live=out[2],
-               workspace=workspace)
+    dev, B, P, n = _pages(page_table, page_refs, stream)
+    if move_src is None and move_dst is None and n_live is None:
+        move_src, move_dst, n_live = \
+            _new((2 * (n // 2) + 1,), torch.int32, dev, stream).split((n // 2, n // 2, 1))
+    else:
+        move_src, move_dst, n_live = (_new((m,), torch.int32, dev, stream) if t is None else t
+                                      for t, m in ((move_src, n // 2), (move_dst, n // 2), (n_live, 1)))
+    at = _ints(dev, (page_table, None, "page_table"), (page_refs, None, "page_refs"),
+               (move_src, n // 2, "move_src"), (move_dst, n // 2, "move_dst"), (n_live, 1, "n_live"))
     workspace, ws, size = _pages_workspace(workspace, n, dev, stream)
     _check("quarot_kv_pages_compact", lib().quarot_kv_pages_compact(*at, B, P, n, ws, size,
                                                                     _stream(stream)))
-    return tuple(out)
+    return move_src, move_dst, n_live
 
 
 def quarot_kv_pages_copy(k_cache, v_cache, src: torch.Tensor, dst: torch.Tensor,
@@ -1287,26 +1304,27 @@ def quarot_kv_pages_copy(k_cache, v_cache, src: torch.Tensor, dst: torch.Tensor,
     kc, ks, kz = k_cache
     vc, vs, vz = v_cache
     _ndim(kc, 4, "k_codes")
-    pages, heads, page, half = kc.shape
     _ndim(ks, 4, "k_scale")
-    if not ks.shape[3]:
-        raise ValueError(f"k_scale must hold groups, got shape {tuple(ks.shape)}")
-    group = 2 * half // ks.shape[3]
-    _group(group, 2 * half)
-    consts = (pages, heads, page, 2 * half // group)
-    _shape(vc, kc.shape, "v_codes")
-    for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
-        _shape(t, consts, nm)
+    pages, heads, page, half = kc.shape
+    groups = ks.shape[3]
+    if not groups or 2 * half % groups:
+        raise ValueError(f"k_scale must hold groups of a row of {2 * half}, got shape {tuple(ks.shape)}")
+    dev = kc.device
+    _on_device(dev, stream)
+    consts, at = (pages, heads, page, groups), []
+    for t, shape, dtype, nm in ((kc, kc.shape, torch.uint8, "k_codes"), (ks, consts, torch.float16, "k_scale"),
+                                (kz, consts, torch.float16, "k_zero"), (vc, kc.shape, torch.uint8, "v_codes"),
+                                (vs, consts, torch.float16, "v_scale"), (vz, consts, torch.float16, "v_zero")):
+        _shape(t, shape, nm)
+        if t.device != dev:
+            _on_device(dev, **{nm: t})
+        at.append(_ptr(t, dtype, nm))
     _ndim(src, 1, "src")
-    _shape(dst, src.shape, "dst")
-    _on_device(kc.device, stream, k_scale=ks, k_zero=kz, v_codes=vc, v_scale=vs, v_zero=vz, src=src, dst=dst)
-    f16 = torch.float16
-    cache = _PagedKV(_ptr(kc, torch.uint8, "k_codes"), _ptr(ks, f16, "k_scale"), _ptr(kz, f16, "k_zero"),
-                     _ptr(vc, torch.uint8, "v_codes"), _ptr(vs, f16, "v_scale"), _ptr(vz, f16, "v_zero"),
-                     None, None, None, 0, heads, 2 * half, group, pages, page, 0)
-    _check("quarot_kv_pages_copy", lib().quarot_kv_pages_copy(
-        ctypes.byref(cache), _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"), src.shape[0],
-        _stream(stream)))
+    count = src.shape[0]
+    lists = _ints(dev, (src, count, "src"), (dst, count, "dst"))
+    cache = _PagedKV(*at, None, None, None, 0, heads, 2 * half, 2 * half // groups, pages, page, 0)
+    _check("quarot_kv_pages_copy", lib().quarot_kv_pages_copy(ctypes.byref(cache), *lists, count,
+                                                              _stream(stream)))
 
 
 def quarot_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,

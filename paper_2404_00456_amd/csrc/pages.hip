@@ -83,43 +83,45 @@ __global__ __launch_bounds__(256) void k_pages_fork(ForkArgs a)
 // at once.
 constexpr int PAGES_EACH = 16;
 
-template <class Test>
-__device__ __forceinline__ int tile_of(const int32_t *refs, int64_t base, int n, uint32_t &yes, Test test)
-{
-    const int64_t first = base + (int64_t)(threadIdx.x >> 6) * 64 * PAGES_EACH;
+struct Tile {
+    int64_t first;  // page of this lane
     int r[PAGES_EACH];
-#pragma unroll
-    for (int k = 0; k < PAGES_EACH; ++k) {
-        const int64_t i = first + 64 * k + (threadIdx.x & 63);
-        r[k] = i < n ? refs[i] : 0;
-    }
-    yes = 0;
-    int count = 0;
-#pragma unroll
-    for (int k = 0; k < PAGES_EACH; ++k) {
-        const int64_t i = first + 64 * k + (threadIdx.x & 63);
-        const bool t = i < n && test((int)i, r[k]);
-        yes |= t ? 1u << k : 0u;
-        count += __builtin_popcountll(__ballot(t));
-    }
-    return count;
-}
 
-// Calls f(page, rank among the tile's) for each page of `yes`; the wave's begin at rank.
-template <class F>
-__device__ __forceinline__ void each_of(int64_t base, uint32_t yes, int rank, F f)
-{
-    const int lane = threadIdx.x & 63;
-    const int64_t first = base + (int64_t)(threadIdx.x >> 6) * 64 * PAGES_EACH;
+    __device__ __forceinline__ Tile(const int32_t *refs, int64_t base, int n)
+    {
+        first = base + (int64_t)(threadIdx.x >> 6) * 64 * PAGES_EACH + (threadIdx.x & 63);
 #pragma unroll
-    for (int k = 0; k < PAGES_EACH; ++k) {
-        const bool t = yes >> k & 1;
-        const uint64_t m = __ballot(t);
-        if (t)
-            f((int)(first + 64 * k + lane), rank + __builtin_popcountll(m & ((1ull << lane) - 1)));
-        rank += __builtin_popcountll(m);
+        for (int k = 0; k < PAGES_EACH; ++k)
+            r[k] = first + 64 * k < n ? refs[first + 64 * k] : 0;
     }
-}
+    template <class Test>
+    __device__ __forceinline__ int count(int n, uint32_t &yes, Test test) const
+    {
+        yes = 0;
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < PAGES_EACH; ++k) {
+            const bool t = first + 64 * k < n && test((int)(first + 64 * k), r[k]);
+            yes |= t ? 1u << k : 0u;
+            count += __builtin_popcountll(__ballot(t));
+        }
+        return count;
+    }
+    // Calls f(page, rank) for each page of `yes`, the wave's first at rank.
+    template <class F>
+    __device__ __forceinline__ void each(uint32_t yes, int rank, F f) const
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll 1
+        for (int k = 0; k < PAGES_EACH; ++k) {  // (its instructions are fetched once)
+            const bool t = yes >> k & 1;
+            const uint64_t m = __ballot(t);
+            if (t)
+                f((int)(first + 64 * k), rank + __builtin_popcountll(m & ((1ull << lane) - 1)));
+            rank += __builtin_popcountll(m);
+        }
+    }
+};
 
 // ---- reserve ----------------------------------------------------------------
 //
@@ -156,6 +158,28 @@ __device__ __forceinline__ Growth growth(const ReserveArgs &a, int b)
     return g;
 }
 
+// Gives back the entries that the wave's sequences shrink out of, 64 of one at a time.
+__device__ __forceinline__ void shrink(const ReserveArgs &a, int b, const Growth &g)
+{
+    const int lane = threadIdx.x & 63;
+    for (uint64_t some = __ballot(g.n < 0 && g.from < g.to); some; some &= some - 1) {
+        const int i = __builtin_ctzll(some), to = __builtin_amdgcn_readlane(g.to, i);
+        int32_t *row = a.table + (int64_t)__builtin_amdgcn_readlane(b, i) * a.P;
+        for (int j = __builtin_amdgcn_readlane(g.from, i) + lane; j < to; j += 64) {
+            const int e = row[j];
+            row[j] = -1;
+            if (is_page(e, a.n))
+                atomicSub(a.refs + e, 1);
+        }
+    }
+}
+
+// What missing[0] says of pages that are lacking.
+__device__ __forceinline__ int lacking(int64_t pages)
+{
+    return (int)min(max(pages, (int64_t)0), (int64_t)0x7FFFFFFF);
+}
+
 // Entry `old` of sequence b as it stands, where it is a page that others hold as well.
 __device__ __forceinline__ int shared_page(const ReserveArgs &a, int b, const Growth &g)
 {
@@ -169,6 +193,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
 {
     __shared__ int at[PAGES_MAX_BATCH];  // fresh pages of the sequences before each
     __shared__ int sums[WAVES];
+    __shared__ int64_t sums8[WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
     int32_t *count = a.ws, *lowest = a.ws + a.n, *list = a.ws + 2 * (int64_t)a.n, *left = a.ws + 3 * (int64_t)a.n;
 
@@ -224,34 +249,35 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
         return mine;
     };
 
-    int total = 0;
-    int64_t rows = 0;
+    int64_t total = 0, rows = 0;
     bool past = false;
     for (int b0 = 0; b0 < a.B; b0 += NT) {
         const int b = b0 + tid;
         const Growth g = growth(a, b);
         int need = copied(b, g) >= 0;
         need += entries(b, g, 0, [](int64_t, int, int) {});
-        int all;
-        const int before = total + block_scan<WAVES>(need, sums, all);
+        int64_t all;
+        const int64_t before = total + block_scan<WAVES>((int64_t)need, sums8, all);
         if (b < a.B)
-            at[b] = before;
+            at[b] = (int)before;
         total += all;
         past |= g.after > (int64_t)a.P * a.page;
         rows += max(0, g.n);
     }
     // (new tokens of all sequences, as a batch has them at most)
-    past |= rows > (1 << 30);
-    past = __syncthreads_or(past);
+    int64_t tokens;
+    block_scan<WAVES>(rows, sums8, tokens);
+    past = __syncthreads_or(past) || tokens > 1 << 30;
 
     int found = 0;
     for (int64_t base = 0; base < a.n && found < total; base += NT * PAGES_EACH) {
+        const Tile tile(a.refs, base, a.n);
         uint32_t yes;
-        const int mine = tile_of(a.refs, base, a.n, yes, [](int, int r) { return r == 0; });
+        const int mine = tile.count(a.n, yes, [](int, int r) { return r == 0; });
         int all;
         // (a wave's count is the same in its lanes: its first lane brings it)
         const int before = block_scan<WAVES>(lane == 0 ? mine : 0, sums, all);
-        each_of(base, yes, found + __builtin_amdgcn_readfirstlane(before), [&](int page, int rank) {
+        tile.each(yes, found + __builtin_amdgcn_readfirstlane(before), [&](int page, int rank) {
             if (rank < total)
                 list[rank] = page;
         });
@@ -291,7 +317,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
     }
     if (tid == 0) {
         a.cu[a.B] = cu;
-        *a.missing = past ? -1 : max(0, total - found);
+        *a.missing = past ? -1 : lacking(total - found);
     }
     if (!done)
         return;
@@ -305,19 +331,152 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
     for (int b0 = 0; b0 < a.B; b0 += NT) {
         const int b = b0 + tid;
         const Growth g = growth(a, b);
-        for (uint64_t some = __ballot(g.n < 0 && g.from < g.to); some; some &= some - 1) {
-            const int i = __builtin_ctzll(some), to = __builtin_amdgcn_readlane(g.to, i);
-            int32_t *row = a.table + (int64_t)__builtin_amdgcn_readlane(b, i) * a.P;
-            for (int j = __builtin_amdgcn_readlane(g.from, i) + lane; j < to; j += 64) {
-                const int e = row[j];
-                row[j] = -1;
-                if (is_page(e, a.n))
-                    atomicSub(a.refs + e, 1);
-            }
-        }
+        shrink(a, b, g);
         if (b < a.B)
             a.lens[b] = (int)g.after;
     }
+}
+
+// The same for batches of a sequence a thread: what was read stays in registers, sharers
+// find each other in a table in LDS, and the first free pages are read while the sequences
+// are.  (64 sequences that grow by a token: 12.4 us by the kernel above; 256 beams, most on
+// a shared page, 21.7.)
+constexpr int SLOTS = 2 * NT;  // of that table
+constexpr int FREE = 2048;     // pages of the list that are kept in LDS
+
+__global__ __launch_bounds__(NT) void k_pages_reserve_few(ReserveArgs a)
+{
+    __shared__ int slot_page[SLOTS], slot_count[SLOTS], slot_lowest[SLOTS];
+    __shared__ int64_t sums[WAVES];
+    __shared__ int sums1[WAVES], near[FREE];
+    const int b = threadIdx.x, lane = b & 63;
+    int32_t *list = a.ws + 2 * (int64_t)a.n, *left = a.ws + 3 * (int64_t)a.n;
+    const Tile head(a.refs, 0, a.n);
+    const Growth g = growth(a, b);
+    // the entry with older tokens, and the first with new ones alone
+    const int64_t row = (int64_t)b * a.P;
+    const bool grows = g.n > 0 && g.from < g.to;
+    const int e0 = g.old >= 0 ? a.table[row + g.old] : -1;
+    const int e1 = grows ? a.table[row + g.from] : -1;
+    const int r0 = is_page(e0, a.n) ? a.refs[e0] : 0, r1 = is_page(e1, a.n) ? a.refs[e1] : 0;
+    for (int i = b; i < SLOTS; i += NT) {
+        slot_page[i] = -1;
+        slot_count[i] = 0;
+        slot_lowest[i] = NT;
+    }
+    __syncthreads();
+    int slot = -1;
+    if (r0 > 1) {  // (a slot is free: there are twice as many as sequences)
+        slot = (uint32_t)e0 * 2654435769u >> 21;
+        static_assert(SLOTS == 1 << 11, "the hash's bits");
+        for (int held; (held = atomicCAS(&slot_page[slot], -1, e0)) != -1 && held != e0;)
+            slot = (slot + 1) % SLOTS;
+        atomicAdd(&slot_count[slot], 1);
+        atomicMin(&slot_lowest[slot], b);
+    }
+    __syncthreads();
+    const bool copies = slot >= 0 && !(slot_count[slot] == r0 && slot_lowest[slot] == b);
+    const bool fresh1 = grows && !(is_page(e1, a.n) && r1 <= 1);
+    // Calls f(index, page or -1, rank) for the needed entries behind the first of each
+    // sequence of the wave's, 64 at a time; the sequence's lane gets how many they were.
+    auto rest = [&](int rank0, auto f) {
+        int mine = 0;
+        for (uint64_t some = __ballot(grows && g.from + 1 < g.to); some; some &= some - 1) {
+            const int i = __builtin_ctzll(some);
+            const int from = __builtin_amdgcn_readlane(g.from, i) + 1, to = __builtin_amdgcn_readlane(g.to, i);
+            const int64_t base = (int64_t)__builtin_amdgcn_readlane(b, i) * a.P;
+            const int first = __builtin_amdgcn_readlane(rank0, i);
+            int rank = first;
+            for (int j0 = from; j0 < to; j0 += 64) {
+                const int j = j0 + lane;
+                const int e = j < to ? a.table[base + j] : -1;
+                const bool page = is_page(e, a.n);
+                const bool need = j < to && !(page && a.refs[page ? e : 0] <= 1);
+                const uint64_t m = __ballot(need);
+                if (need)
+                    f(base + j, page ? e : -1, rank + __builtin_popcountll(m & ((1ull << lane) - 1)));
+                rank += __builtin_popcountll(m);
+            }
+            mine += lane == i ? rank - first : 0;
+        }
+        return mine;
+    };
+    const int need = copies + fresh1 + rest(0, [](int64_t, int, int) {});
+    int64_t total, tokens;
+    const int mine = (int)block_scan<WAVES>((int64_t)need, sums, total);
+    const int cu = (int)block_scan<WAVES>((int64_t)max(0, g.n), sums, tokens);
+    const bool past = __syncthreads_or(g.after > (int64_t)a.P * a.page) || tokens > 1 << 30;
+
+    int found = 0;
+    for (int64_t base = 0; base < a.n && found < total; base += NT * PAGES_EACH) {
+        const Tile tile = base ? Tile(a.refs, base, a.n) : head;
+        uint32_t yes;
+        const int count = tile.count(a.n, yes, [](int, int r) { return r == 0; });
+        int some;
+        const int first = found + __builtin_amdgcn_readfirstlane(block_scan<WAVES>(lane == 0 ? count : 0, sums1, some));
+        if (first < total)
+            tile.each(yes, first, [&](int page, int rank) {
+                if (rank < FREE)
+                    near[rank] = page;
+                else if (rank < total)
+                    list[rank] = page;
+            });
+        found += some;
+    }
+    const bool done = !past && found >= total;
+    __syncthreads();
+    auto page_of = [&](int rank) { return rank < FREE ? near[rank] : list[rank]; };
+    int rank = mine, dst = -1, page1 = -1;
+    if (done) {
+        if (copies) {
+            dst = page_of(rank++);
+            a.table[row + g.old] = dst;
+        }
+        if (fresh1) {
+            page1 = page_of(rank++);
+            a.table[row + g.from] = page1;
+        }
+        rest(rank, [&](int64_t i, int was, int r) {
+            a.table[i] = page_of(r);
+            left[r] = was;
+        });
+    }
+    if (b < a.B) {
+        a.cu[b] = done ? cu : 0;
+        a.src[b] = dst >= 0 ? e0 : -1;
+        a.dst[b] = dst;
+    }
+    if (b == 0) {
+        a.cu[a.B] = done ? (int)tokens : 0;
+        *a.missing = past ? -1 : lacking(total - found);
+    }
+    if (!done)
+        return;
+    __syncthreads();  // references change once all have been read
+    if (dst >= 0) {
+        put(a.refs + dst, 1);
+        atomicSub(a.refs + e0, 1);
+    }
+    if (page1 >= 0) {
+        put(a.refs + page1, 1);
+        if (is_page(e1, a.n))
+            atomicSub(a.refs + e1, 1);
+    }
+    // the others, by their ranks: those behind each sequence's own two
+    const int own = copies + fresh1;
+    for (uint64_t some = __ballot(need > own); some; some &= some - 1) {
+        const int i = __builtin_ctzll(some);
+        const int first = __builtin_amdgcn_readlane(mine + own, i), end = __builtin_amdgcn_readlane(mine + need, i);
+        for (int r = first + lane; r < end; r += 64) {
+            put(a.refs + page_of(r), 1);
+            const int was = left[r];
+            if (was >= 0)
+                atomicSub(a.refs + was, 1);
+        }
+    }
+    shrink(a, b, g);
+    if (b < a.B)
+        a.lens[b] = (int)g.after;
 }
 
 // ---- compact ----------------------------------------------------------------
@@ -328,41 +487,45 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(ReserveArgs a)
 __global__ __launch_bounds__(NT) void k_pages_compact(CompactArgs a)
 {
     __shared__ int sums[WAVES];
+    __shared__ int64_t sums2[WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
+    const Tile head(a.refs, 0, a.n);
     int live = 0;
     for (int64_t base = 0; base < a.n; base += NT * PAGES_EACH) {
+        const Tile tile = base ? Tile(a.refs, base, a.n) : head;
         uint32_t yes;
-        const int mine = tile_of(a.refs, base, a.n, yes, [](int, int r) { return r > 0; });
+        const int mine = tile.count(a.n, yes, [](int, int r) { return r > 0; });
         int all;
         block_scan<WAVES>(lane == 0 ? mine : 0, sums, all);
         live += all;
     }
-    int nsrc = 0, ndst = 0;
+    int64_t pairs = 0;  // sources below, destinations from bit 32 on
     for (int64_t base = 0; base < a.n; base += NT * PAGES_EACH) {
+        const Tile tile = base ? Tile(a.refs, base, a.n) : head;
         uint32_t from, to;
-        const int ms = tile_of(a.refs, base, a.n, from, [&](int i, int r) { return r > 0 && i >= live; });
-        const int md = tile_of(a.refs, base, a.n, to, [&](int i, int r) { return r <= 0 && i < live; });
-        int alls, alld;
-        const int bs = block_scan<WAVES>(lane == 0 ? ms : 0, sums, alls);
-        const int bd = block_scan<WAVES>(lane == 0 ? md : 0, sums, alld);
-        each_of(base, from, nsrc + __builtin_amdgcn_readfirstlane(bs), [&](int p, int r) { a.src[r] = p; });
-        each_of(base, to, ndst + __builtin_amdgcn_readfirstlane(bd), [&](int p, int r) { a.dst[r] = p; });
-        nsrc += alls;
-        ndst += alld;
+        const int64_t ms = tile.count(a.n, from, [&](int i, int r) { return r > 0 && i >= live; });
+        const int64_t md = tile.count(a.n, to, [&](int i, int r) { return r <= 0 && i < live; });
+        int64_t all;
+        const int64_t before = pairs + block_scan<WAVES>(lane == 0 ? ms | md << 32 : 0, sums2, all);
+        const int bs = __builtin_amdgcn_readfirstlane((int)before), bd = __builtin_amdgcn_readfirstlane((int)(before >> 32));
+        tile.each(from, bs, [&](int p, int r) { a.src[r] = p; });
+        tile.each(to, bd, [&](int p, int r) { a.dst[r] = p; });
+        pairs += all;
     }
+    const int moves = (int)pairs;
     for (int64_t i = live + tid; i < a.n; i += NT)
         a.ws[i] = (int)i;
+    for (int i = moves + tid; i < a.n / 2; i += NT)
+        a.src[i] = a.dst[i] = -1;
     if (tid == 0)
         *a.live = live;
     __syncthreads();
-    for (int i = tid; i < nsrc; i += NT) {
+    for (int i = tid; i < moves; i += NT) {
         const int s = a.src[i], d = a.dst[i];
         a.ws[s] = d;
         a.refs[d] = a.refs[s];
         a.refs[s] = 0;
     }
-    for (int i = nsrc + tid; i < a.n / 2; i += NT)
-        a.src[i] = a.dst[i] = -1;
 }
 
 __global__ __launch_bounds__(256) void k_pages_follow(CompactArgs a)
@@ -432,7 +595,10 @@ hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t s)
 
 hipError_t launch_pages_reserve(const ReserveArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(NT), 0, s, a);
+    if (a.B <= NT)
+        hipLaunchKernelGGL(k_pages_reserve_few, dim3(1), dim3(NT), 0, s, a);
+    else
+        hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
 

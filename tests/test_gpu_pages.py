@@ -237,3 +237,19 @@ def test_another_stream(dev):
     x.p.fork([0, 0, 1])
     x.same()
     assert got[0].tolist() == [0, 17, 22, 22]
+
+
+@pytest.mark.parametrize("B", [3, 1500])
+def test_new_tokens_of_a_batch(dev, B):
+    """More than 2^30 new tokens are refused, however few each sequence has."""
+    import torch
+    import paper_2404_00456_amd as q
+    table = torch.full((B, 1), -1, dtype=torch.int32, device=dev)
+    lens, refs = ints([0] * B, dev), ints([0] * 8, dev)
+    page = 1 << 29
+    new = ints([page] * 3 + [0] * (B - 3), dev)
+    cu, src, dst, missing = q.quarot_kv_pages_reserve(table, lens, refs, new, page)
+    assert missing.item() == -1 and not cu.any() and not lens.any() and (table == -1).all()
+    new[0] = 0
+    cu, src, dst, missing = q.quarot_kv_pages_reserve(table, lens, refs, new, page)
+    assert missing.item() == 0 and cu[-1].item() == 2 * page and lens.tolist()[:4] == [0, page, page, 0][:min(4, B)]
