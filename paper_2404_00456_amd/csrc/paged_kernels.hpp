@@ -110,9 +110,9 @@ __device__ __forceinline__ View view_span(const typename M::Args &a, const Work 
     v.low = a.window > 0 ? p - a.window + 1 : 0;
     v.high = p + 1;
     if constexpr (M::SCORED) {
-        v.low = max(v.low, a.begin ? a.begin[trow] : 0);
-        if (a.end)
-            v.high = max(0, min(a.end[trow], w.len));
+        // (no negative ones, which a query before the first position would have)
+        v.low = max(max(v.low, 0), a.begin ? a.begin[trow] : 0);
+        v.high = max(a.end ? min(a.end[trow], w.len) : v.high, 0);
     }
     return v;
 }
