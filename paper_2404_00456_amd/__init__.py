@@ -1199,12 +1199,19 @@ def _ints(dev, *named):
     for t, n, name in named:
         if not isinstance(t, torch.Tensor) or t.dtype != i32 or t.device != dev or \
                 not t.is_contiguous() or not t.is_cuda or (n is not None and t.shape != (n,)):
-            _ptr(t, i32, name)
-            if n is not None:
-                _shape(t, (n,), name)
-            _on_device(dev, **{name: t})
+            break
         at.append(t.data_ptr())
-    return at
+    else:
+        return at
+    for t, n, name in named:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if n is not None:
+            _shape(t, (n,), name)
+    for t, _, name in named:
+        _ptr(t, i32, name)
+        _on_device(dev, **{name: t})
+    raise ValueError("the tensors changed while they were looked at")
 
 
 def _pages(page_table, page_refs, stream):
@@ -1309,18 +1316,21 @@ def quarot_kv_pages_copy(k_cache, v_cache, src: torch.Tensor, dst: torch.Tensor,
     groups = ks.shape[3]
     if not groups or 2 * half % groups:
         raise ValueError(f"k_scale must hold groups of a row of {2 * half}, got shape {tuple(ks.shape)}")
+    _ndim(src, 1, "src")
+    count = src.shape[0]
+    _shape(dst, (count,), "dst")
     dev = kc.device
     _on_device(dev, stream)
     consts, at = (pages, heads, page, groups), []
-    for t, shape, dtype, nm in ((kc, kc.shape, torch.uint8, "k_codes"), (ks, consts, torch.float16, "k_scale"),
-                                (kz, consts, torch.float16, "k_zero"), (vc, kc.shape, torch.uint8, "v_codes"),
-                                (vs, consts, torch.float16, "v_scale"), (vz, consts, torch.float16, "v_zero")):
-        _shape(t, shape, nm)
+    _shape(vc, kc.shape, "v_codes")
+    for t, nm in ((ks, "k_scale"), (kz, "k_zero"), (vs, "v_scale"), (vz, "v_zero")):
+        _shape(t, consts, nm)
+    for t, dtype, nm in ((kc, torch.uint8, "k_codes"), (ks, torch.float16, "k_scale"),
+                         (kz, torch.float16, "k_zero"), (vc, torch.uint8, "v_codes"),
+                         (vs, torch.float16, "v_scale"), (vz, torch.float16, "v_zero")):
         if t.device != dev:
             _on_device(dev, **{nm: t})
         at.append(_ptr(t, dtype, nm))
-    _ndim(src, 1, "src")
-    count = src.shape[0]
     lists = _ints(dev, (src, count, "src"), (dst, count, "dst"))
     cache = _PagedKV(*at, None, None, None, 0, heads, 2 * half, 2 * half // groups, pages, page, 0)
     _check("quarot_kv_pages_copy", lib().quarot_kv_pages_copy(ctypes.byref(cache), *lists, count,
@@ -1338,8 +1348,6 @@ def quarot_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[t
     _ndim(logits, 2, "logits")
     if logits.dtype not in (torch.float16, torch.float32):
         raise TypeError(f"logits must be {torch.float16} or {torch.float32}, got {logits.dtype}")
-    if not logits.is_cuda:
-        raise ValueError("logits must be a device tensor")
     rows, V = logits.shape
     stride = logits.stride(0) if rows > 1 else V
     if V > 1 and logits.stride(1) != 1:
@@ -1349,10 +1357,12 @@ def quarot_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[t
     for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p),
                     ("min_p", min_p), ("tokens", tokens)):
         _shape(t, (rows,), name)
-    _on_device(logits.device, stream, u=u, temperature=temperature, top_k=top_k, top_p=top_p,
-               min_p=min_p, tokens=tokens)
     if u is None:
         raise TypeError("u must be a torch.Tensor")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    _on_device(logits.device, stream, u=u, temperature=temperature, top_k=top_k, top_p=top_p,
+               min_p=min_p, tokens=tokens)
     if tokens is None:
         tokens = _new((rows,), torch.int32, logits.device, stream)
     f32, i32 = torch.float32, torch.int32
