@@ -1033,7 +1033,9 @@ def _paged_kv(k_cache, v_cache, page_table, seq_lens, cu_new, group: int, rows: 
                          (cu_new, i32, "cu_new")):
         if t.device != dev:
             raise ValueError(f"{nm} must be on {dev}, got {t.device}")
-        at.append(_ptr(t, dtype, nm))
+        if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+            _ptr(t, dtype, nm)
+        at.append(t.data_ptr())
     _on_device(dev)
     return _PagedKV(*at, B, heads, 2 * half, group, pages, page, most)
 
@@ -1131,8 +1133,8 @@ def _paged_attention(q, k_cache, v_cache, page_table, seq_lens, cu_new, group, w
         out = _new((T, H, D), torch.float16, q.device, stream)
     (qp, qs), (op, ost) = _token_rows(q, "q"), _token_rows(out, "out")
     if workspace is None:
-        need = quarot_kv_paged_attention_workspace_size(
-            T, cache.batch, H, cache.n_kv_heads, D, max_seq_len, window, n_sinks, group)
+        need = lib().quarot_kv_paged_attention_workspace_size(
+            T, cache.batch, H, cache.n_kv_heads, D, group, max_seq_len, window, n_sinks)
         if need:
             workspace = _new((need,), torch.uint8, q.device, stream)
     head = (qp, qs, op, ost, ctypes.byref(cache))

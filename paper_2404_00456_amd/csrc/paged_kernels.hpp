@@ -973,11 +973,12 @@ __global__ __launch_bounds__(64 * NW)
         constexpr int H = 64 / TS;      // stages of a step
         constexpr int PM = Sh::PAIRS / KS;  // pairs with a part
         const NibConst nk = nib_const();
-        // first token of stage j; past the last one, the last one again.  Where scores fall
-        // by distance the nearest come first: from far to near, a steep slope moved the
-        // reference in every round (a prompt of 8192, 2351 us).
+        // first token of stage j; past the last one, the last one again.  Scored forms take
+        // the nearest first: from far to near, a steep slope moved the reference in every
+        // round (a prompt of 8192, 2351 us instead of 1320), and the exact rounds at the end
+        // of a span do better beside the first loads (documents 279 us, 270 so).
         auto token0 = [&](int j) {
-            const int last = (end - begin) * H - 1, k = M::BIAS ? max(last - j, 0) : min(j, last);
+            const int last = (end - begin) * H - 1, k = M::SCORED ? max(last - j, 0) : min(j, last);
             return paged::step_token(w, begin + k / H) + k % H * TS;
         };
         spoiled[wave] = 0;
