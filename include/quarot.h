@@ -768,7 +768,8 @@ quarot_status quarot_kv_pages_copy(const quarot_paged_kv *cache, const int32_t *
  * weights passes u times their total, for a given random number 0 <= u < 1 (others are
  * taken as 0, or as the last kept token).  T <= 0 (or not a number): the token of the
  * largest logit, the lowest such.  Logits of -inf or that are no number are never chosen;
- * a row of nothing else gives -1.  A logit of +inf counts as the largest binary32 number.
+ * a row of nothing else gives -1.  A logit of +inf weighs as much as the largest binary32
+ * number and comes before it.
  * Weights are rounded to multiples of 2^-min(51, 62 - ceil(log2 vocab)) and summed
  * exactly, so that the result does not depend on the order of any sum.
  *   logits [rows, vocab], `stride` elements between rows, binary16 (f32 == 0) or binary32,

@@ -12,17 +12,18 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     out = []
     for r in range(rows):
         x = logits[r].astype(np.float64)
-        x = np.minimum(np.where(np.isnan(x), -np.inf, x), float(np.finfo(np.float32).max))
-        m = x.max()
+        x = np.where(np.isnan(x), -np.inf, x)
+        best = int(np.argmax(x))
+        order = np.argsort(-x, kind="stable")
+        x = np.minimum(x, float(np.finfo(np.float32).max))
+        m = x[best]
         if m == -np.inf:
             out.append(-1)
             continue
-        best = int(np.argmax(x))
         t = 1.0 if temperature is None else float(temperature[r])
         if not t > 0:
             out.append(best)
             continue
-        order = np.argsort(-x, kind="stable")
         order = order[x[order] > -np.inf]
         k = 0 if top_k is None else int(top_k[r])
         if k > 0:

@@ -144,6 +144,34 @@ def test_flat_rows_use_every_level(dev):
             check(dev, x, rng.random(rows), top_k=[V // 2] * rows, top_p=[0.9] * rows, min_p=[0.9] * rows, **kw)
 
 
+def test_infinite_beside_the_largest_number(dev):
+    """They weigh the same, and the infinite ones come first."""
+    inf, big = np.float32(np.inf), np.finfo(np.float32).max
+    x = np.tile(np.array([1.0, big, inf, big, inf, -inf, big], np.float32), (8, 300))
+    u = (np.arange(8) + 0.5) / 8
+    for kw in ({}, dict(temperature=[0.0] * 8), dict(top_k=[1, 2, 3, 599, 600, 601, 1500, 0]),
+               dict(top_p=[1e-6, 0.1, 0.3, 0.4, 0.41, 0.7, 0.99, 1.0]), dict(min_p=[0.5] * 8)):
+        check(dev, x, u, **kw)
+
+
+@pytest.mark.parametrize("V", [600, 30000])
+def test_cuts_at_logits_near_zero(dev, V):
+    """Where the least logit of a step of the exponent is next to 0 a rounding of the largest
+    logit is billions of numbers there."""
+    rng = np.random.default_rng(V)
+    rows, steps = 12, 8 * 40 + 7.5
+    x = (rng.standard_normal((rows, V)) * 10.0 ** rng.integers(-30, -6, (rows, V))).astype(np.float32)
+    x[:, V // 2] = 1.0
+    T = 256 / np.log(2) / steps
+    share = 1 / (1 + V * np.exp(-1 / T))  # of the one token
+    p = share + (1 - share) * rng.random(rows)
+    for t in (T, T * (1 + 1e-6), T * (1 - 1e-6)):
+        kw = dict(temperature=[t] * rows)
+        check(dev, x, rng.random(rows), top_p=p, **kw)
+        check(dev, x, rng.random(rows), min_p=np.exp(-1 / t) * (1 + rng.standard_normal(rows) * 1e-7), **kw)
+        check(dev, x, rng.random(rows), top_p=p, top_k=rng.integers(1, V, rows), **kw)
+
+
 def test_frequencies(dev):
     """Evenly spaced random numbers give each token its share of them, to one."""
     import torch
