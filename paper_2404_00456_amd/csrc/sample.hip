@@ -786,6 +786,8 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
     if (p < 1.0f && listed) {
         c = by_logit(s, (int)n, row.V, low, high, weight, [&](u64 all) { return share_of(p, all); });
     } else if (p < 1.0f) {
+        const int nothing = -(a.log2_one + 2) * STEPS;  // (less weighs nothing)
+        static_assert(53 * STEPS / 8 < BINS, "their bins");
         clear(s);
         for (int i = threadIdx.x; i < BINS; i += NT)
             s.count[i] = 0;
@@ -795,13 +797,13 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     int step;
-                    u64 x = w.whole(l[e], step);
+                    const u64 x = w.whole(l[e], step);
+                    bool some = step >= nothing;
                     if (exact)
-                        x &= c.keeps(l[e], row.index(t, e)) ? ~0ull : 0;
-                    if (x) {
-                        const int b = w.bin_of_step(step);
-                        atomicAdd(&s.bins[b], x);
-                        atomicAdd(&s.count[b], 1u);
+                        some &= c.keeps(l[e], row.index(t, e));
+                    if (some) {
+                        atomicAdd(&s.bins[-step >> 3], x);
+                        atomicAdd(&s.count[-step >> 3], 1u);
                     }
                 }
             });
