@@ -1825,13 +1825,20 @@ template <int D, int MR, class M>
 hipError_t go_combine(const typename M::Args &a, int slots, hipStream_t s)
 {
     const unsigned x = (unsigned)(slots * a.hkv);
+    // Rows of a block row are shared by blocks: of few rows, by two blocks of eight (16 in
+    // one block: 8 sequences of 4096 19 us instead of 18) or one for each row of a token and
+    // more; of a tile, by so many that 2048 blocks are there, down to a row a wave (with 4 a
+    // query head, six prompts of some 200 over 6302 tokens and 2 heads in 25 splits 161
+    // us, 14 so).
+    auto blocks = [&](int least, int each) {
+        return MR == paged::FEW_ROWS ? (unsigned)least
+                                     : (unsigned)std::min(MR / each, std::max<int>(least, (int)(2048 / x)));
+    };
     if (a.splits > 8)
-        hipLaunchKernelGGL((k_paged_combine<D, MR, 4, M>), dim3(x, (unsigned)std::min(MR, a.rep * 4)),
+        hipLaunchKernelGGL((k_paged_combine<D, MR, 4, M>), dim3(x, blocks(std::min(MR, a.rep * 4), 1)),
                            dim3(256), 0, s, a);
     else
-        // rows of a block row are shared by blocks of eight (16 in one block: 8
-        // sequences of 4096 19 us instead of 18)
-        hipLaunchKernelGGL((k_paged_combine<D, MR, 1, M>), dim3(x, MR == paged::FEW_ROWS ? 2 : MR / 32),
+        hipLaunchKernelGGL((k_paged_combine<D, MR, 1, M>), dim3(x, blocks(MR == paged::FEW_ROWS ? 2 : MR / 32, 4)),
                            dim3(256), 0, s, a);
     return hipGetLastError();
 }
