@@ -133,6 +133,20 @@ def test_longer_ones_of_normal_rows(dev, D, G, new, total, form):
     check(dev, bt, bt.queries(2, 2.0), exact=False, max_seq_len=max(total), **kw)
 
 
+@pytest.mark.parametrize("hkv,rep,D,G", [(1, 1, 128, 128), (2, 1, 64, 32), (1, 3, 256, 256), (3, 2, 128, 32)])
+@pytest.mark.parametrize("form", ["cap", "any"])
+def test_many_splits_of_few_heads(dev, hkv, rep, D, G, form):
+    """Rows of a tile whose splits are joined by blocks of a few rows each; the last tile
+    of a sequence is partly rows of nobody."""
+    f = dict(FORMS[form])
+    new, total = [300, 33, 1, 129], [2900, 700, 500, 1600]
+    bt = Batch(11, new, total, hkv, D, G, 16, behind=2, exact=False)
+    kw = dict(cap=f.get("cap", 0.0), sinks=3)
+    if "spans" in f:
+        kw["begin"], kw["end"] = spans(bt, f["spans"])
+    check(dev, bt, bt.queries(hkv * rep, 2.0), exact=False, max_seq_len=max(total), **kw)
+
+
 def test_no_form_is_the_plain_attention(dev):
     """No cap, no slopes, no spans: few rows bit for bit, tiles within their roundings;
     slopes of 0 and spans of the causal order change nothing."""
