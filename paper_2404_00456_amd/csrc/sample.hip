@@ -8,7 +8,7 @@
 // their total.
 //
 // Weights are whole numbers, rint(w 2^log2_one) from a binary64 exponential (relative
-// error below 1e-13), and all sums are sums of those: exact, whatever their order, and so
+// error below 2e-13), and all sums are sums of those: exact, whatever their order, and so
 // is every decision.  2^log2_one lets the sum of a vocabulary stay below 2^63 (a
 // vocabulary of 2^17: 2^45), so that a weight that becomes 0 is below 2^-46 of the
 // largest.
