@@ -1669,22 +1669,68 @@ __global__ __launch_bounds__(64 * ROWS_W)
 
     if constexpr (NG > 1) {
         // Values that only some rows see have to be finite (weights of one group's rows
-        // are masked row by row instead).  All waves look at all of them: no more than
-        // 15 behind the first row's position, and as many where windows begin (in spans
-        // of a form, as many as those differ by).  (Looked at where they pass through,
-        // single tokens, which have none, took 41 us instead of 39.)
+        // are masked row by row instead).  Without spans all waves look at all of them: no
+        // more than 15 behind the first row's position, and as many where windows begin.
+        // (Looked at where they pass through, single tokens, which have none, took 41 us
+        // instead of 39.)  Spans may differ by any number of tokens, and where each begins
+        // and ends is known by their reach alone (`every`, `after`): each wave looks at those
+        // of its own stages, by groups of 16 tokens.  (4 tokens over 30100, 8 heads, groups
+        // of 32: begins 30000 apart 31 us, 26 alike; all of them looked at by each wave,
+        // 662.)
         if (pmin != pmax) {
             const typename M::Args again = args_again<typename M::Args>();
-            const int behind = M::SCORED ? w.hi - 1 - every : pmax - pmin;
-            const int before = M::SCORED ? max(0, min(w.hi, after + 1) - w.low) : again.window > 0 ? behind : 0;
-            bool odd = false;
-            for (int64_t i = lane; i < (int64_t)(behind + before) * NG; i += 64) {
-                const int j = (int)(i / NG);
-                const int t = j < behind ? every + 1 + j : after - (j - behind);
-                const int64_t at = pool_row(again.map, again.hkv, w.b, t);
-                const int64_t gi = (at + (int64_t)pl.h * again.map.page) * NG + (int)(i % NG);
-                if (at >= 0 && t < w.hi)
-                    odd |= (spoils(again.vp.s[gi], again.vp.z[gi]) & 0x8000u) != 0;
+            bool odd = false, spans = false;
+            if constexpr (M::SCORED) {
+                spans = again.begin || again.end;
+                constexpr int LPG = 2 * NG, AT_ONCE = 64 / LPG;  // lanes of a group, of 16 bytes each
+                for (int k = 0; spans && k < stages; k += 32) {
+                    if (stages > 32)  // (else they are those that the first look found)
+                        look(k);
+                    const int t0 = token_at(min(k + (lane >> 1), stages - 1)) + 16 * (lane & 1);
+                    const uint64_t part = __ballot(base >= 0 && (t0 + 15 > every || t0 <= after));
+                    for (uint64_t left = part; left;) {
+                        const int x0 = __builtin_ctzll(left) / AT_ONCE * AT_ONCE;
+                        left &= ~(((1ull << AT_ONCE) - 1) << x0);
+                        const int x = x0 + lane / LPG, c = lane % LPG * 8;
+                        const int t = __shfl(t0, x) + c / NG;
+                        const int64_t gi = (int64_t)((uint64_t)(uint32_t)__shfl((int)(base >> 32), x) << 32 |
+                                                     (uint32_t)__shfl((int)base, x)) * NG + c;
+                        if (part >> x & 1) {
+                            const uint4 s4 = *reinterpret_cast<const uint4 *>(again.vp.s + gi);
+                            const uint4 z4 = *reinterpret_cast<const uint4 *>(again.vp.z + gi);
+                            const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const int tt = t + 2 * y / NG;
+                                const bool some = tt < w.hi && (tt >= w.low || tt < again.sinks);
+                                const bool all = tt <= every && (tt > after || tt < again.sinks);
+                                odd |= some && !all && spoils(s[y], z[y]) != 0;
+                            }
+                        }
+                    }
+                }
+                if (spans) {
+                    // told to the other waves through the first word of each one's ring
+                    auto told = [&](int v) { return reinterpret_cast<int *>(lds + v * (ROWS_NS * Ring::STAGE)); };
+                    odd = __any(odd);
+                    if (lane == 0)
+                        *told(wave) = odd;
+                    __syncthreads();
+#pragma unroll
+                    for (int v = 0; v < ROWS_W; ++v)
+                        odd |= *told(v) != 0;
+                }
+            }
+            if (!spans) {
+                const int behind = pmax - pmin, of = (again.window > 0 ? 2 : 1) * behind * NG;
+                for (int i = lane; i < of; i += 64) {
+                    const int j = i / NG;
+                    const int t = j < behind ? pmin + 1 + j : pmax - again.window - (j - behind);
+                    const int64_t at = pool_row(again.map, again.hkv, w.b, t);
+                    const int64_t gi = (at + (int64_t)pl.h * again.map.page) * NG + i % NG;
+                    if (at >= 0 && t < w.hi)
+                        odd |= (spoils(again.vp.s[gi], again.vp.z[gi]) & 0x8000u) != 0;
+                }
             }
             if (__any(odd)) {
                 for (int r = wave; r < R; r += ROWS_W)
