@@ -67,9 +67,10 @@ struct Plain {
 // With X the score in log2 units (sm_scale log2(e) q . khat):
 //   X <- c tanh(X / c) = c - 2 c / (1 + 2^(X 2 log2(e) / c)),  c = cap log2(e)      (CAP)
 //   X <- X - slope log2(e) (|p - t| - d)                                            (BIAS)
-// d is the distance of the nearest token that the query sees: a constant of its row,
-// which no softmax changes, and without which a query that sees only far tokens would
-// take its weights from the last bits of large numbers.
+// d is the distance of the token that it favours most of those that the query sees, the
+// nearest one (with a slope below 0 the farthest): a constant of its row, which no softmax
+// changes, and without which the weights would come from the last bits of large numbers
+// where that token is far away.
 // c - 2 c / (1 + e) is off by some 2^-23 c, whatever the score is: 2e-5 log2 units for a
 // cap of 128.  Caps beyond CAP_LARGE are forms of their own, which take scores below an
 // eighth of them by the series of tanh instead (its next term is 1.3e-9 of the score there).
@@ -96,7 +97,7 @@ struct Work : paged::Span {
 
 // What a query at position p of batch row trow sees (low <= t < high, and the sinks
 // before high), and how its scores fall: by slope for each position from p further than
-// near.
+// near (d above).
 struct View {
     int p, low, high, near;
     float slope;  // in log2 units
@@ -122,9 +123,15 @@ __device__ __forceinline__ View view(const typename M::Args &a, const Work &w, i
 {
     View v = view_span<M>(a, w, trow, p);
     if constexpr (M::BIAS) {
-        const int last = v.low < v.high ? min(max(p, v.low), v.high - 1) : min(a.sinks, v.high) - 1;
-        v.near = abs(p - last);
-        v.slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
+        v.slope = a.slopes[head] * LOG2E;
+        const bool far = v.slope < 0.0f;
+        auto distance = [&](int from, int to) {  // of that token among from .. to
+            const int nearest = min(max(p, from), to), farthest = p - from > to - p ? from : to;
+            return abs(p - (far ? farthest : nearest));
+        };
+        const int span = distance(min(v.low, v.high - 1), v.high - 1);
+        const int sinks = min(a.sinks, v.high), sink = distance(0, sinks - 1);
+        v.near = v.low >= v.high ? sink : sinks <= 0 ? span : far ? max(span, sink) : min(span, sink);
     }
     return v;
 }
@@ -1268,12 +1275,12 @@ __global__ __launch_bounds__(64 * ROWS_W)
         const int r = w.row0 + min(m, R - 1), i = r / a.rep;
         return view<M>(a, w, w.tok0 + i, w.pos0 + i, pl.h * a.rep + (r - i * a.rep));
     };
-    float fall = 0.0f;  // of a score, for each position before the nearest that is seen
-    int nearest = 0;
+    float fall = 0.0f;  // of a score, for each position before `favoured` (p less d)
+    int favoured = 0;
     if constexpr (M::BIAS) {
         const View v = viewed();
         fall = v.slope;
-        nearest = v.p - v.near;
+        favoured = v.p - v.near;
     }
     uint4 qraw[KW];
     {
@@ -1428,7 +1435,7 @@ __global__ __launch_bounds__(64 * ROWS_W)
         if constexpr (M::BIAS) {
             exact |= th + 31 > pmin;
             slope = fall;
-            off = __builtin_fmaf(slope, (float)(th + 4 * g - nearest), off);
+            off = __builtin_fmaf(slope, (float)(th + 4 * g - favoured), off);
         }
         if (FORM && exact)
             off = slope = 0.0f;
