@@ -294,7 +294,7 @@ struct Weights {
     __device__ __forceinline__ int bin_of(float l) const
     {
         const float x = l >= m ? 0.0f : (m - l) * bin;
-        return x < (float)BINS ? (int)x : BINS;  // (0 times infinite: BINS)
+        return x < (float)BINS ? (int)x : BINS;  // (what is no number: BINS)
     }
 };
 
@@ -711,7 +711,9 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
     Weights w;
     w.m = std::min(m, MOST);
     w.step = STEPS * 1.44269504088896340736 / (double)temp;
-    w.bin = (float)(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp);
+    // (at most what binary32 holds: at temperatures below 2e-37 the bins are wider, and what
+    // lies past the last of them still weighs nothing)
+    w.bin = (float)std::min(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp, (double)MOST);
     w.pow2 = s.pow2;
     __syncthreads();
 
