@@ -293,7 +293,8 @@ struct Weights {
     // Bins of the logits: equal steps down to weights of 0, which are BINS and more.
     __device__ __forceinline__ int bin_of(float l) const
     {
-        const float x = l >= m ? 0.0f : (m - l) * bin;
+        // (by halves of the logits, whose difference is always a number)
+        const float x = l >= m ? 0.0f : __builtin_fmaf(l, -0.5f, 0.5f * m) * (2.0f * bin);
         return x < (float)BINS ? (int)x : BINS;  // (what is no number: BINS)
     }
 };
@@ -713,7 +714,7 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
     w.step = STEPS * 1.44269504088896340736 / (double)temp;
     // (at most what binary32 holds: at temperatures below 2e-37 the bins are wider, and what
     // lies past the last of them still weighs nothing)
-    w.bin = (float)std::min(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp, (double)MOST);
+    w.bin = (float)std::min(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp, 0.5 * MOST);
     w.pow2 = s.pow2;
     __syncthreads();
 

@@ -1,5 +1,5 @@
 """Sampling on the GPU at temperatures near the ends of binary32, where a step of a histogram
-is no binary32 number any more."""
+or a difference of logits is no binary32 number any more."""
 import numpy as np
 import pytest
 
@@ -33,4 +33,24 @@ def test_temperatures_as_small_as_the_logits_differ(dev, V, T):
     # beside logits of ordinary size, which weigh nothing
     x[:, ::3] = rng.standard_normal((rows, len(x[0, ::3]))) - 9
     for k in (2, 50, V // 2, V - 1):
+        check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
+
+
+@pytest.mark.parametrize("V", [3001, 30000])
+@pytest.mark.parametrize("T", [1e37, 1e38, 3e38])
+def test_logits_further_apart_than_the_largest_number(dev, V, T):
+    rng = np.random.default_rng(V)
+    rows = 16
+    x = (rng.uniform(-3.3e38, 3.3e38, (rows, V))).astype(np.float32)
+    x[:, ::7] = -np.inf
+    x[:, 1::50] = np.nan
+    kw = dict(temperature=[T] * rows)
+    for k in (2, 50, 1500, V // 2, V - 1):
+        check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
+        check(dev, x, rng.random(rows), top_k=[k] * rows, top_p=[0.7] * rows, **kw)
+    # one far above all others
+    x[:, 5] = 3.4e38
+    x[:, 6:] = np.minimum(x[:, 6:], -3e38)
+    x[:, :5] = -3e38
+    for k in (2, 50, 1500, V // 2):
         check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
