@@ -683,8 +683,9 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
             a.tokens[r] = -1;
         return;
     }
-    const float temp = a.temperature ? std::min(a.temperature[r], MOST) : 1.0f;
-    if (!(temp > 0.0f)) {
+    // (infinite: as a number that leaves every finite logit its whole weight)
+    const double temp = std::min(a.temperature ? (double)a.temperature[r] : 1.0, 0x1p1000);
+    if (!(temp > 0.0)) {
         if (threadIdx.x == 0)
             s.token = a.V;
         __syncthreads();
@@ -711,10 +712,10 @@ __global__ __launch_bounds__(NT) void k_sample(SampleArgs a)
     }
     Weights w;
     w.m = std::min(m, MOST);
-    w.step = STEPS * 1.44269504088896340736 / (double)temp;
+    w.step = STEPS * 1.44269504088896340736 / temp;
     // (at most what binary32 holds: at temperatures below 2e-37 the bins are wider, and what
     // lies past the last of them still weighs nothing)
-    w.bin = (float)std::min(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / (double)temp, 0.5 * MOST);
+    w.bin = (float)std::min(BINS / ((a.log2_one + 1.5) * 0.693147180559945309417) / temp, 0.5 * MOST);
     w.pow2 = s.pow2;
     __syncthreads();
 

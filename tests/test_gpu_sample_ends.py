@@ -54,3 +54,24 @@ def test_logits_further_apart_than_the_largest_number(dev, V, T):
     x[:, :5] = -3e38
     for k in (2, 50, 1500, V // 2):
         check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
+
+
+@pytest.mark.parametrize("V", [3001, 30000])
+def test_an_infinite_temperature(dev, V):
+    """Every finite logit weighs the same, whatever their size."""
+    rng = np.random.default_rng(V)
+    rows = 16
+    x = (rng.uniform(-3.3e38, 3.3e38, (rows, V))).astype(np.float32)
+    x[:, ::7] = -np.inf
+    x[:, 1::50] = np.nan
+    kw = dict(temperature=[np.inf] * rows)
+    check(dev, x, rng.random(rows), **kw)
+    for k in (2, 1500, V // 2):
+        check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
+    check(dev, x, rng.random(rows), top_p=[0.7] * rows, **kw)
+    for p in (0.5, 1.0):
+        check(dev, x, rng.random(rows), min_p=[p] * rows, **kw)
+    # two infinite ones weigh as the others
+    x[:, [3, V - 2]] = np.inf
+    for k in (0, 1, 2, 3, V // 2):
+        check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
