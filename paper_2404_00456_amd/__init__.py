@@ -1183,8 +1183,8 @@ def quarot_kv_paged_attention_scored(q: torch.Tensor, k_cache, v_cache, page_tab
     [T], positions of their sequence; None: 0, and causal).  Documents packed in a
     sequence begin where they do; tokens of a prefix that see each other have its
     length as end, where that is past their own position."""
-    for t, n, name in ((slopes, q.shape[1] if q.dim() == 3 else -1, "slopes"),
-                       (begin, q.shape[0], "begin"), (end, q.shape[0], "end")):
+    _half_rows(q, "q")
+    for t, n, name in ((slopes, q.shape[1], "slopes"), (begin, q.shape[0], "begin"), (end, q.shape[0], "end")):
         if t is not None:
             _shape(t, (n,), name)
     _on_device(k_cache[0].device, stream, slopes=slopes, begin=begin, end=end)
