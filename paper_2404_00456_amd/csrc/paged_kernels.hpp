@@ -823,7 +823,7 @@ __global__ __launch_bounds__(64 * NW)
     if constexpr (M::CAP) {
         top = M::LARGE ? 0.0f : a.cap * LOG2E;
         times = M::LARGE ? 1.0f : -2.0f * top;
-        ck = c2 * (2.0f / a.cap);
+        ck = fminf(c2 * (2.0f / a.cap), 0x1.FFFFFEp127f);  // (infinite, it would leave no 0)
     }
     auto ready = [&](v16f &s, int r) {
         if constexpr (M::LARGE)
