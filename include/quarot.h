@@ -666,8 +666,10 @@ quarot_status quarot_kv_paged_attention(const quarot_f16 *q, int64_t q_stride, q
  * Neither changes with the other: a query with begin[r] >= end[r] sees its sinks, or
  * nothing and gives zeros.  All three arrays lie on the device and are read when the
  * kernels run; any content of begin and end is in bounds.
- * All else is as in quarot_kv_paged_attention, the workspace (and its query) as well.
- * cap 0 (none) or 2^-64 .. 2^64.
+ * All else is as in quarot_kv_paged_attention, the workspace (and its query) as well, and
+ * so is what is rounded: at most 16 query rows a sequence with one group a row give outputs
+ * off by their own rounding, 2e-4 of their size on average, other calls by 4e-4 to 7e-4
+ * (more where scores are large).  cap 0 (none) or 2^-64 .. 2^64.
  */
 typedef struct quarot_scoring {
     float cap;
@@ -758,7 +760,7 @@ quarot_status quarot_kv_pages_copy(const quarot_paged_kv *cache, const int32_t *
  * ---- Sampling -------------------------------------------------------------------
  *
  * The next token of each row of logits.  With m the row's largest logit and T its
- * temperature, a token's weight is w = exp((l - m) / T).  Tokens are put in the order of
+ * temperature (it may be infinite), a token's weight is w = exp((l - m) / T).  Tokens are put in the order of
  * their logits, the lower index first where they are equal, and
  *   top_k > 0   keeps the first top_k,
  *   top_p < 1   of those the shortest beginning whose weights sum up to top_p of theirs

@@ -29,7 +29,7 @@
 //
 // What bounds it: instructions, of 131072 tokens a microsecond for each one a token of the
 // row's CU.  A pass for the largest logit or for a list is a handful (two fp16 at once, or
-// groups that hold none left out), weighing a token 30, 12 of them in binary64.  All of it is
+// groups that hold none left out), weighing a token 32 to 40, 13 of them in binary64.  All of it is
 // inlined: where a function took the row or the cut by reference they lived in scratch memory,
 // and the loops waited for all their loads at each use (a share of 0.98 of 50003 tokens, 61 us
 // before and 42 without; conditions as masks of a wave, no branches or selects, 39).
