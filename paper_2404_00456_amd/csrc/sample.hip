@@ -78,16 +78,17 @@ struct Shared {
 
 constexpr float MOST = 0x1.FFFFFEp127f;
 
-// Whole numbers in the order of the logits.
+// Whole numbers in the order of the logits, one for each number: with a number for -0 of
+// its own, the one before that of 0 would be no smaller logit.
 __device__ __forceinline__ uint32_t key_of(float l)
 {
     const uint32_t b = __float_as_uint(l + 0.0f);  // (no -0)
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    return b & 0x80000000u ? 0u - b : b | 0x80000000u;
 }
 
 __device__ __forceinline__ float of_key(uint32_t k)
 {
-    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : 0u - k);
 }
 
 template <class T>

@@ -75,3 +75,43 @@ def test_an_infinite_temperature(dev, V):
     x[:, [3, V - 2]] = np.inf
     for k in (0, 1, 2, 3, V // 2):
         check(dev, x, rng.random(rows), top_k=[k] * rows, **kw)
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("V", [600, 11505, 60000])
+@pytest.mark.parametrize("T", [1e-40, 1e-30, 1e-20, 1.0])
+def test_the_largest_logits_are_zeros(dev, V, T, dtype):
+    """More equal ones than a list holds, where the next logit below is a subnormal number."""
+    rng = np.random.default_rng(V)
+    rows = 8
+    x = np.zeros((rows, V), dtype)
+    x[::2, ::3] = -0.0
+    x[4:, 1::2] = -np.inf
+    x[6:, ::5] = -rng.integers(1, 9, x[6:, ::5].shape) * float(np.finfo(dtype).smallest_subnormal)
+    kw = dict(temperature=[T] * rows)
+    for mp in (1.0, 0.9, 1e-9):
+        check(dev, x, rng.random(rows), min_p=[mp] * rows, **kw)
+        check(dev, x, rng.random(rows), min_p=[mp] * rows, top_k=[V // 3] * rows, **kw)
+    for p in (0.1, 0.9):
+        check(dev, x, rng.random(rows), top_p=[p] * rows, **kw)
+        check(dev, x, rng.random(rows), top_p=[p] * rows, top_k=[V // 3] * rows, **kw)
+
+
+@pytest.mark.parametrize("few", [False, True])
+def test_a_step_of_the_histogram_ends_at_zero(dev, few):
+    """At this temperature a step of the first histogram reaches from the largest logit down
+    to 0, and the next one begins at the number below it."""
+    least, V, rows = 2.0 ** -149, 60000, 8
+    rng = np.random.default_rng(7)
+    x = np.full((rows, V), -np.inf, np.float32)
+    for r in range(rows):
+        at = rng.permutation(V)[:V // 6 if few else V]
+        n = len(at) // 3
+        x[r, at[:n]] = rng.choice([0.0, -0.0], n)
+        x[r, at[n:]] = -least * rng.integers(1, 1000, len(at) - n)
+        x[r, at[-1]] = 4445110 * least
+    T = [3.874576352977353e-37] * rows
+    n = np.isfinite(x[0]).sum()
+    for k in (n // 3, n // 3 + 1, n // 3 + 2, n // 2, n - 1):
+        check(dev, x, rng.random(rows), temperature=T, top_k=[k] * rows)
+        check(dev, x, rng.random(rows), temperature=T, top_k=[k] * rows, top_p=[0.8] * rows)
